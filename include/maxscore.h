@@ -342,6 +342,62 @@ int32_t maxscore_combine(const void *expert_out, int32_t in_dtype, const int32_t
                          const float *gates, int32_t T, int32_t d, int32_t E, int32_t k, int32_t C, float *y,
                          void *stream);
 
+/* The experts' own products, between maxscore_dispatch_tokens and maxscore_combine, and the way back from the layer's result.
+ *
+ * Buffers are [E, C, width] as maxscore_dispatch_tokens fills them: expert j's rows are the first
+ * n_j = expert_offsets[j+1] - expert_offsets[j] (cut off at 0 and C) of its C places.  Places from n_j on are never used on the way in, whatever
+ * they hold, and are zero on the way out.  E <= 1024, C <= 2^21, widths (K, N, d) <= 2^20, any of them odd; rows that are whole numbers of 16 bytes
+ * in 16-byte aligned buffers take the fast path.  Sums are held in fp32 and rounded once.  All of these calls only enqueue work, use no
+ * workspace and may be captured into a graph; results do not depend on what else runs.
+ *
+ * maxscore_expert_matmul: y[j, s, :] = x[j, s, :] . W[j].  x [E, C, K], y [E, C, N] and W are of in_dtype (bf16 or fp32); W is [E, K, N], or with
+ * transposed != 0 [E, N, K].  The gradient with respect to x is the same call on dy with the other value of `transposed`.
+ *
+ * maxscore_expert_matmul_wgrad: dW[j] = sum_s x[j, s, :]^T dy[j, s, :], [E, K, N] (zero for an expert without rows).  x [E, C, K] and dy [E, C, N] are
+ * of in_dtype, dW is fp32 or, for bf16 inputs, bf16 (out_dtype).  The gradient of a transposed W is the call with x and dy, K and N exchanged.
+ *
+ * maxscore_expert_swiglu: the gated unit [g | u] = x[j, s, :] . W[j], h[j, s, :] = u * g / (1 + e^-g).  W is [E, K, 2N] (transposed: [E, 2N, K]), gate
+ * columns first; h [E, C, N]; gate_up [E, C, 2N] receives [g | u] and may be NULL.  h is made from the sums before they are rounded.
+ *
+ * maxscore_expert_swiglu_backward: from gate_up and dh [E, C, N] (in_dtype, as are the results) dgate_up [E, C, 2N]:
+ *   s = 1 / (1 + e^-g),  dg = dh * u * s * (1 + g * (1 - s)),  du = dh * g * s;  h (may be NULL) receives u * g * s again.
+ *
+ * maxscore_combine_backward: the gradients of maxscore_combine with respect to the experts' rows and the gates, from dy [T, d] (fp32):
+ *   dexpert_out[assign[i, s], token_pos[i, s], :] = gates[i, s] * dy[i, :],   dgates[i, s] = <dy[i, :], expert_out[assign[i, s], token_pos[i, s], :]>.
+ * expert_out and dexpert_out [E, C, d] are of in_dtype.  Slots with assign < 0 or a place outside the buffer have dgates 0.  assign, token_pos and
+ * expert_offsets are one dispatch's.  (The gradient of maxscore_dispatch_tokens is maxscore_combine of the buffers' gradient with gates of 1.) */
+int32_t maxscore_expert_matmul(const void *x, const void *W, int32_t in_dtype, int32_t transposed, const int32_t *expert_offsets,
+                               int32_t E, int32_t C, int32_t K, int32_t N, void *y, void *stream);
+int32_t maxscore_expert_matmul_wgrad(const void *x, const void *dy, int32_t in_dtype, const int32_t *expert_offsets, int32_t E,
+                                     int32_t C, int32_t K, int32_t N, int32_t out_dtype, void *dW, void *stream);
+int32_t maxscore_expert_swiglu(const void *x, const void *W, int32_t in_dtype, int32_t transposed, const int32_t *expert_offsets,
+                               int32_t E, int32_t C, int32_t K, int32_t N, void *h, void *gate_up, void *stream);
+int32_t maxscore_expert_swiglu_backward(const void *gate_up, const void *dh, int32_t in_dtype, const int32_t *expert_offsets,
+                                        int32_t E, int32_t C, int32_t N, void *dgate_up, void *h, void *stream);
+int32_t maxscore_combine_backward(const float *dy, const void *expert_out, int32_t in_dtype, const int32_t *assign,
+                                  const int32_t *token_pos, const float *gates, const int32_t *expert_offsets, int32_t T, int32_t d,
+                                  int32_t E, int32_t k, int32_t C, void *dexpert_out, float *dgates, void *stream);
+
+/* The same products in microscaled four-bit numbers, for serving.  A row of d values (d a multiple of 32) is d/2 bytes of codes, two to a byte, the first
+ * one in the low bits, and d/32 bytes of scales: every 32 values share 2^(byte - 127); a code is a sign bit above the index of
+ * {0, 1/2, 1, 3/2, 2, 3, 4, 6}.
+ *
+ * maxscore_mxfp4_quantise: x [rows, d] (bf16 or fp32) into q [rows, d/2] and scales [rows, d/32].  A block's power of two is
+ * 2^(floor(log2 m) - 2) for its largest magnitude m, at least 2^-127 (also for a block of zeros); values are rounded to the nearest, ties to the even
+ * code, and what lies beyond 6 times the power of two becomes 6 of it.  A block that holds an infinity or a NaN gets the scale byte 255 (NaN throughout).
+ * maxscore_mxfp4_dequantise: the values, exact in fp32 and bf16.
+ *
+ * maxscore_expert_matmul_mxfp4: y [E, C, N] (bf16) = xq . Wq^T per expert, x [E, C, K] and W [E, N, K] in that form.
+ * maxscore_expert_swiglu_mxfp4: h [E, C, N] (bf16) of the gated unit, W [E, 2N, K].  Rows in four bits are dispatched by maxscore_dispatch_tokens as rows
+ * of d/4 (codes) and, where d is a multiple of 64, d/64 (scales) values of 16 bits. */
+int32_t maxscore_mxfp4_quantise(const void *x, int32_t in_dtype, int64_t rows, int32_t d, void *q, void *scales, void *stream);
+int32_t maxscore_mxfp4_dequantise(const void *q, const void *scales, int64_t rows, int32_t d, int32_t out_dtype, void *x,
+                                  void *stream);
+int32_t maxscore_expert_matmul_mxfp4(const void *xq, const void *xs, const void *Wq, const void *Ws, const int32_t *expert_offsets,
+                                     int32_t E, int32_t C, int32_t K, int32_t N, void *y, void *stream);
+int32_t maxscore_expert_swiglu_mxfp4(const void *xq, const void *xs, const void *Wq, const void *Ws, const int32_t *expert_offsets,
+                                     int32_t E, int32_t C, int32_t K, int32_t N, void *h, void *stream);
+
 /* a2..a6 from given logits.  scores_out[T,E] and q_out[T,E] are required (they are the working
  * storage of a2/a3).  Synchronises `stream`. */
 int32_t maxscore_route_logits(const float *logits, int32_t T, int32_t E, int32_t k, int32_t C,

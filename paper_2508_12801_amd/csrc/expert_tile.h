@@ -1,0 +1,299 @@
+// Matrix products of the experts' rows, one tile of one expert's result to a workgroup.
+//
+//   D[m, n] = sum_k A(m, k) B(n, k)
+//
+// An operand is "rows" (k contiguous in memory: x[rows, K], W[E, N, K]) or "cols" (k is the row index: W[E, K, N]; both operands of the
+// weight gradient, where k counts the expert's rows).  k is walked in slabs of 128 bytes of an operand's row: 64 bf16, 32 fp32, 256 four-bit
+// numbers.  A slab of R rows takes R * 128 bytes of LDS either way, in 16-byte chunks:
+//   rows  row r, chunk c at r * 128 + 16 * (c ^ (r & 7)): eight rows' chunks of one column lie in eight different places of 128 bytes
+//   cols  k's row of R elements, chunk c at k * R * size + 16 * (c ^ turn(k)), where turn spreads four rows over 256 bytes
+// and is read in the layout of 32x32 matrix instructions: lane l has row l % 32 of a block and chunk 4 * (l / 32) + kk of the slab in step kk.
+// Which of the slab's k a lane has in a step does not matter as long as both operands agree.  Operands that are cols come through LDS's
+// transposing reads (bf16: four k of sixteen rows at a time) or word by word (fp32, whose matrix instructions take eight times as long).
+// B is the instruction's first operand, so that a lane ends with four neighbouring columns n of one row m.
+#pragma once
+#include "expert_steps.h"
+
+namespace maxscore {
+
+namespace {
+
+typedef unsigned int ex_u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int ex_u32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((ext_vector_type(8))) __bf16 ex_bf16x8;
+typedef __attribute__((ext_vector_type(4))) __bf16 ex_bf16x4;
+typedef __attribute__((ext_vector_type(16))) float ex_f32x16;
+typedef __attribute__((ext_vector_type(4))) float ex_f32x4;
+typedef __attribute__((ext_vector_type(8))) int ex_i32x8;
+
+constexpr int kSlabBytes = 128;
+
+// Elements of a format to 16 bytes, and bits of one.
+template <int F> struct ExpertElem;
+template <> struct ExpertElem<kExpBf16> { static constexpr int chunk = 8; };
+template <> struct ExpertElem<kExpFp32> { static constexpr int chunk = 4; };
+template <> struct ExpertElem<kExpMx> { static constexpr int chunk = 32; };
+
+__device__ __forceinline__ unsigned short ex_to_bf16(float v)      // to nearest, ties to even
+{
+    return __builtin_bit_cast(unsigned short, (__bf16)v);
+}
+
+// 16 bytes of elements col .. of row `row` of a matrix of `cols` columns, zero where the matrix has none.
+template <int F, bool ALIGNED>
+__device__ __forceinline__ ex_u32x4 ex_load16(const char *base, int row, int col, int rows, int cols)
+{
+    constexpr int CE = ExpertElem<F>::chunk;
+    ex_u32x4 v = {0u, 0u, 0u, 0u};
+    if (row >= rows || col >= cols) return v;
+    const char *p = base + ((size_t)row * cols + col) * 16 / CE;
+    if (ALIGNED) return *(const ex_u32x4 *)p;          // rows are whole numbers of chunks then
+    if constexpr (F == kExpFp32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (col + i < cols) v[i] = ((const unsigned *)p)[i];
+    } else if constexpr (F == kExpBf16) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (col + i < cols) v[i / 2] |= (unsigned)((const unsigned short *)p)[i] << (i % 2 * 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i / 4] |= (unsigned)((const unsigned char *)p)[i] << (i % 4 * 8);
+    }
+    return v;
+}
+
+// How far the chunks of row k of a slab of cols are turned.
+template <int F, int R>
+__device__ __forceinline__ int ex_turn(int k)
+{
+    if constexpr (F != kExpBf16 || R < 64) return 0;
+    else if constexpr (R == 64) return (k >> 1 & 1) << 2;
+    else return (k & 3) << 2;
+}
+
+// Place of chunk q (in the order of LDS) in the slab: row and column of the operand's tile, column in elements.
+template <int F, bool COLS, int R>
+__device__ __forceinline__ void ex_place(int q, int &row, int &col)
+{
+    constexpr int CE = ExpertElem<F>::chunk;
+    if constexpr (!COLS) {
+        row = q >> 3;
+        col = ((q & 7) ^ (row & 7)) * CE;
+    } else {
+        constexpr int CPR = R / CE;
+        row = q / CPR;
+        col = ((q % CPR) ^ ex_turn<F, R>(row)) * CE;
+    }
+}
+
+template <int F> struct ExpertFrag;
+template <> struct ExpertFrag<kExpBf16> { ex_bf16x8 v; };
+template <> struct ExpertFrag<kExpFp32> { ex_f32x4 v; };
+template <> struct ExpertFrag<kExpMx> { ex_u32x4 v; };
+
+// A lane's part of block `rb` (32 rows) of an operand in step kk.
+template <int F, bool COLS, int R>
+__device__ __forceinline__ ExpertFrag<F> ex_fragment(const char *slab, int rb, int kk, int lane)
+{
+    ExpertFrag<F> f;
+    const int c = 4 * (lane >> 5) + kk;
+    if constexpr (!COLS) {
+        const int r = rb * 32 + (lane & 31);
+        const ex_u32x4 v = *(const ex_u32x4 *)(slab + r * kSlabBytes + ((c ^ (r & 7)) << 4));
+        f.v = __builtin_bit_cast(decltype(f.v), v);
+    } else if constexpr (F == kExpBf16) {
+        typedef __attribute__((address_space(3))) ex_bf16x4 *lds_quad;
+        const int n = rb * 32 + (lane >> 4 & 1) * 16 + (lane & 3) * 4, k = 8 * c + ((lane & 15) >> 2);
+        const char *p0 = slab + k * (R * 2) + (((n >> 3) ^ ex_turn<F, R>(k)) << 4) + (n & 7) * 2;
+        const char *p1 = slab + (k + 4) * (R * 2) + (((n >> 3) ^ ex_turn<F, R>(k + 4)) << 4) + (n & 7) * 2;
+        const ex_bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_quad)p0), hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_quad)p1);
+        f.v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+        const int n = rb * 32 + (lane & 31);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f.v[i] = *(const float *)(slab + ((4 * c + i) * R + n) * 4);
+    }
+    return f;
+}
+
+// acc[n, m] += B A of one step.  sb, sa: the lane's scales of the slab, a byte a step (four bits).
+template <int F, int KK>
+__device__ __forceinline__ ex_f32x16 ex_mma(const ExpertFrag<F> &b, const ExpertFrag<F> &a, ex_f32x16 acc, int sb, int sa)
+{
+    if constexpr (F == kExpBf16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(b.v, a.v, acc, 0, 0, 0);
+    else if constexpr (F == kExpFp32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(b.v[i], a.v[i], acc, 0, 0, 0);
+        return acc;
+    } else {
+        const ex_i32x8 bv = {(int)b.v[0], (int)b.v[1], (int)b.v[2], (int)b.v[3], 0, 0, 0, 0};
+        const ex_i32x8 av = {(int)a.v[0], (int)a.v[1], (int)a.v[2], (int)a.v[3], 0, 0, 0, 0};
+        return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(bv, av, acc, 4, 4, KK, sb, KK, sa);
+    }
+}
+
+// u * g / (1 + e^-g).  Where e^-g is infinite the quotient is zero, as it should be.
+__device__ __forceinline__ float ex_silu_times(float g, float u) { return u * (g / (1.f + expf(-g))); }
+
+// Four neighbouring columns of a row of the result, in the type of the result.
+template <bool FP32, bool ALIGNED>
+__device__ __forceinline__ void ex_store4(void *out, size_t at, int left, const float (&v)[4])
+{
+    if constexpr (FP32) {
+        float *p = (float *)out + at;
+        if (ALIGNED) *(ex_f32x4 *)p = ex_f32x4{v[0], v[1], v[2], v[3]};
+        else
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < left) p[i] = v[i];
+    } else {
+        unsigned short *p = (unsigned short *)out + at;
+        if (ALIGNED)
+            *(ex_u32x2 *)p = ex_u32x2{ex_to_bf16(v[0]) | (unsigned)ex_to_bf16(v[1]) << 16, ex_to_bf16(v[2]) | (unsigned)ex_to_bf16(v[3]) << 16};
+        else
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < left) p[i] = ex_to_bf16(v[i]);
+    }
+}
+
+// WM x WN wavefronts, each with TM x TN blocks of 32 x 32.  The gated unit takes gate and up columns by turns of 32, so that a wavefront
+// has both of an h in the same lane and register.
+template <int F, bool COLS_B, bool WGRAD, int END, bool ALIGNED, int WM, int WN, int TM, int TN>
+__global__ __launch_bounds__(64 * WM * WN) void k_expert_product(ExpertArgs p)
+{
+    constexpr int NT = 64 * WM * WN, BM = 32 * WM * TM, BN = 32 * WN * TN, CE = ExpertElem<F>::chunk, KS = kSlabBytes / 16 * CE;
+    constexpr bool GATED = END == kExpSwiglu || END == kExpSwigluKeep, OUT32 = F == kExpFp32 || END == kExpStoreFp32, MX = F == kExpMx;
+    constexpr bool COLS_A = WGRAD;
+    static_assert(!GATED || TN % 2 == 0, "gate and up in one wavefront");
+    __shared__ __attribute__((aligned(128))) char s_a[BM * kSlabBytes], s_b[BN * kSlabBytes];
+    __shared__ unsigned char s_sa[MX ? BM * 8 : 1], s_sb[MX ? BN * 8 : 1];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / WN, wn = wave % WN;
+
+    const int per = p.mt * p.nt, j = blockIdx.x / per, t = blockIdx.x - j * per;
+    const int m0 = t / p.nt * BM, n0 = t % p.nt * (GATED ? BN / 2 : BN);
+    const int o0 = p.offsets[j], cnt = p.offsets[j + 1] - o0, filled = cnt < 0 ? 0 : cnt < p.C ? cnt : p.C;
+    const int ms = WGRAD ? p.M : filled, ks = WGRAD ? filled : p.K;           // rows of the result that have sums, length of these
+    const int n_all = GATED ? 2 * p.N : p.N;
+
+    // row (or column, of cols) of B's matrix that the tile's column c is
+    auto b_index = [&](int c) { return GATED ? (n0 + (c >> 6) * 32 + (c & 31) < p.N ? n0 + (c >> 6) * 32 + (c & 31) + (c & 32 ? p.N : 0) : n_all) : n0 + c; };
+
+    ex_f32x16 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int u = 0; u < TN; ++u)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][u][e] = 0.f;
+
+    if (m0 < ms) {
+        const size_t row_a = (size_t)(WGRAD ? p.M : p.K) * 16 / CE;
+        const char *a = (const char *)p.a + (size_t)j * p.C * row_a;
+        const char *b = (const char *)p.b + (WGRAD ? (size_t)j * p.C * p.N : (size_t)j * n_all * p.K) * 16 / CE;
+        const unsigned char *sa = MX ? p.sa + (size_t)j * p.C * (p.K / 32) : nullptr, *sb = MX ? p.sb + (size_t)j * n_all * (p.K / 32) : nullptr;
+        for (int k0 = 0; k0 < ks; k0 += KS) {
+            __syncthreads();
+#pragma unroll
+            for (int q = tid; q < BM * 8; q += NT) {
+                int row, col;
+                ex_place<F, COLS_A, BM>(q, row, col);
+                *(ex_u32x4 *)(s_a + q * 16) = COLS_A ? ex_load16<F, ALIGNED>(a, k0 + row, m0 + col, ks, p.M) : ex_load16<F, ALIGNED>(a, m0 + row, k0 + col, ms, p.K);
+            }
+#pragma unroll
+            for (int q = tid; q < BN * 8; q += NT) {
+                int row, col;
+                ex_place<F, COLS_B, BN>(q, row, col);
+                *(ex_u32x4 *)(s_b + q * 16) = COLS_B ? ex_load16<F, ALIGNED>(b, k0 + row, b_index(col), ks, n_all) : ex_load16<F, ALIGNED>(b, b_index(row), k0 + col, n_all, p.K);
+            }
+            if constexpr (MX) {
+                const int blocks = p.K / 32, k32 = k0 / 32;
+                for (int q = tid; q < BM * 8; q += NT) s_sa[q] = m0 + (q >> 3) < ms && k32 + (q & 7) < blocks ? sa[(size_t)(m0 + (q >> 3)) * blocks + k32 + (q & 7)] : 0;
+                for (int q = tid; q < BN * 8; q += NT) s_sb[q] = b_index(q >> 3) < n_all && k32 + (q & 7) < blocks ? sb[(size_t)b_index(q >> 3) * blocks + k32 + (q & 7)] : 0;
+            }
+            __syncthreads();
+            int va[TM], vb[TN];
+#pragma unroll
+            for (int i = 0; i < TM; ++i) va[i] = MX ? *(const int *)(s_sa + (wm * TM * 32 + i * 32 + (lane & 31)) * 8 + 4 * (lane >> 5)) : 0;
+#pragma unroll
+            for (int u = 0; u < TN; ++u) vb[u] = MX ? *(const int *)(s_sb + (wn * TN * 32 + u * 32 + (lane & 31)) * 8 + 4 * (lane >> 5)) : 0;
+            auto step = [&](auto kk) {
+                constexpr int KK = decltype(kk)::value;
+                ExpertFrag<F> fa[TM], fb[TN];
+#pragma unroll
+                for (int i = 0; i < TM; ++i) fa[i] = ex_fragment<F, COLS_A, BM>(s_a, wm * TM + i, KK, lane);
+#pragma unroll
+                for (int u = 0; u < TN; ++u) fb[u] = ex_fragment<F, COLS_B, BN>(s_b, wn * TN + u, KK, lane);
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int u = 0; u < TN; ++u) acc[i][u] = ex_mma<F, KK>(fb[u], fa[i], acc[i][u], vb[u], va[i]);
+            };
+            step(std::integral_constant<int, 0>{});
+            step(std::integral_constant<int, 1>{});
+            step(std::integral_constant<int, 2>{});
+            step(std::integral_constant<int, 3>{});
+        }
+    }
+
+    // rows of the buffer that hold nothing are zero
+    const size_t out0 = (size_t)j * p.M * p.N, keep0 = (size_t)j * p.M * n_all;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int m = m0 + (wm * TM + i) * 32 + (lane & 31);
+        if (m >= p.M) continue;
+        const bool has = m < ms;
+#pragma unroll
+        for (int u = 0; u < TN; u += GATED ? 2 : 1)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int n = n0 + (GATED ? (wn * TN + u) * 16 : (wn * TN + u) * 32) + 8 * q + 4 * (lane >> 5), left = p.N - n;
+                if (left <= 0) continue;
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = has ? acc[i][u][4 * q + e] : 0.f;
+                if constexpr (GATED) {
+                    float w[4], h[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = has ? acc[i][u + 1][4 * q + e] : 0.f;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) h[e] = ex_silu_times(v[e], w[e]);
+                    ex_store4<OUT32, ALIGNED>(p.out, out0 + (size_t)m * p.N + n, left, h);
+                    if constexpr (END == kExpSwigluKeep) {
+                        ex_store4<OUT32, ALIGNED>(p.keep, keep0 + (size_t)m * n_all + n, left, v);
+                        ex_store4<OUT32, ALIGNED>(p.keep, keep0 + (size_t)m * n_all + p.N + n, left, w);
+                    }
+                } else {
+                    ex_store4<OUT32, ALIGNED>(p.out, out0 + (size_t)m * p.N + n, left, v);
+                }
+            }
+    }
+}
+
+template <int F, bool COLS_B, bool WGRAD, int END, bool ALIGNED, int WM, int WN, int TM, int TN>
+int32_t ex_launch(ExpertArgs p, hipStream_t s)
+{
+    constexpr bool GATED = END == kExpSwiglu || END == kExpSwigluKeep;
+    constexpr int BM = 32 * WM * TM, BN = 32 * WN * TN / (GATED ? 2 : 1);
+    p.mt = (p.M + BM - 1) / BM;
+    p.nt = (p.N + BN - 1) / BN;
+    const long long tiles = (long long)p.mt * p.nt * p.E;
+    if (tiles > 0xffffffffll / (64 * WM * WN)) return MAXSCORE_ERR_SHAPE;      // a launch counts its threads in 32 bits
+    hipLaunchKernelGGL((k_expert_product<F, COLS_B, WGRAD, END, ALIGNED, WM, WN, TM, TN>), dim3((unsigned)tiles), dim3(64 * WM * WN), 0, s, p);
+    MS_HIP(hipGetLastError());
+    return MAXSCORE_OK;
+}
+
+// Whether all rows of the operands and the results begin on 16 bytes and are whole numbers of them.
+template <int F>
+bool ex_aligned(const ExpertArgs &p, bool cols_b, bool wgrad)
+{
+    constexpr int CE = ExpertElem<F>::chunk;
+    const uintptr_t at = (uintptr_t)p.a | (uintptr_t)p.b | (uintptr_t)p.out | (uintptr_t)p.keep;
+    if (at % 16 || p.N % (F == kExpMx ? 8 : CE)) return false;
+    return wgrad ? p.M % CE == 0 : p.K % CE == 0;
+}
+
+}  // namespace
+}  // namespace maxscore
