@@ -9,8 +9,11 @@ namespace {
 template <bool COLS_B, bool WGRAD, int END>
 int32_t run(const ExpertArgs &p, hipStream_t s)
 {
-    if (ex_aligned<kExpBf16>(p, COLS_B, WGRAD)) return ex_launch<kExpBf16, COLS_B, WGRAD, END, true, 2, 2, 2, 2>(p, s);
-    return ex_launch<kExpBf16, COLS_B, WGRAD, END, false, 2, 2, 2, 2>(p, s);
+    if (ex_aligned<kExpBf16>(p, COLS_B, WGRAD, END == kExpSwiglu || END == kExpSwigluKeep)) {
+        if (p.M <= 128) return ex_launch<kExpBf16, COLS_B, WGRAD, END, true, 2, 2, 2, 2, 2>(p, s);
+        return ex_launch<kExpBf16, COLS_B, WGRAD, END, true, 2, 4, 4, 2, 1>(p, s);
+    }
+    return ex_launch<kExpBf16, COLS_B, WGRAD, END, false, 2, 2, 2, 2, 2>(p, s);
 }
 
 }  // namespace

@@ -9,8 +9,8 @@ namespace {
 template <bool COLS_B, bool WGRAD, int END>
 int32_t run(const ExpertArgs &p, hipStream_t s)
 {
-    if (ex_aligned<kExpFp32>(p, COLS_B, WGRAD)) return ex_launch<kExpFp32, COLS_B, WGRAD, END, true, 2, 2, 2, 2>(p, s);
-    return ex_launch<kExpFp32, COLS_B, WGRAD, END, false, 2, 2, 2, 2>(p, s);
+    if (ex_aligned<kExpFp32>(p, COLS_B, WGRAD, END == kExpSwiglu || END == kExpSwigluKeep)) return ex_launch<kExpFp32, COLS_B, WGRAD, END, true, 2, 2, 2, 2, 2>(p, s);
+    return ex_launch<kExpFp32, COLS_B, WGRAD, END, false, 2, 2, 2, 2, 2>(p, s);
 }
 
 }  // namespace

@@ -9,8 +9,8 @@ namespace {
 template <int END>
 int32_t run(const ExpertArgs &p, hipStream_t s)
 {
-    if (ex_aligned<kExpMx>(p, false, false)) return ex_launch<kExpMx, false, false, END, true, 2, 2, 2, 2>(p, s);
-    return ex_launch<kExpMx, false, false, END, false, 2, 2, 2, 2>(p, s);
+    if (ex_aligned<kExpMx>(p, false, false, END == kExpSwiglu)) return ex_launch<kExpMx, false, false, END, true, 2, 2, 2, 2, 2>(p, s);
+    return ex_launch<kExpMx, false, false, END, false, 2, 2, 2, 2, 2>(p, s);
 }
 
 }  // namespace

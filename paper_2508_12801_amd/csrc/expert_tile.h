@@ -63,6 +63,14 @@ __device__ __forceinline__ ex_u32x4 ex_load16(const char *base, int row, int col
     return v;
 }
 
+// 16 bytes a lane from base + off straight into LDS, a wavefront's 1024 bytes behind each other from `lds` on.  Not waited for: what
+// reads them comes behind ex_loads_done and a barrier.
+__device__ __forceinline__ void ex_load_lds(const char *base, unsigned off, unsigned lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ void ex_loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 // How far the chunks of row k of a slab of cols are turned.
 template <int F, int R>
 __device__ __forceinline__ int ex_turn(int k)
@@ -160,16 +168,21 @@ __device__ __forceinline__ void ex_store4(void *out, size_t at, int left, const 
 
 // WM x WN wavefronts, each with TM x TN blocks of 32 x 32.  The gated unit takes gate and up columns by turns of 32, so that a wavefront
 // has both of an h in the same lane and register.
-template <int F, bool COLS_B, bool WGRAD, int END, bool ALIGNED, int WM, int WN, int TM, int TN>
-__global__ __launch_bounds__(64 * WM * WN) void k_expert_product(ExpertArgs p)
+//
+// Two slabs in LDS: the next one is on its way, past the registers, while the matrix instructions work on this one, and one barrier a slab keeps them
+// apart.  A slab that ends early, and every slab of rows that are no whole numbers of 16 bytes, is filled in through registers, zero where there is nothing;
+// rows and columns of the tile that the result does not have are copies of its last ones.
+template <int F, bool COLS_B, bool WGRAD, int END, bool ALIGNED, int WM, int WN, int TM, int TN, int WGS>
+__global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_product(ExpertArgs p)
 {
     constexpr int NT = 64 * WM * WN, BM = 32 * WM * TM, BN = 32 * WN * TN, CE = ExpertElem<F>::chunk, KS = kSlabBytes / 16 * CE;
     constexpr bool GATED = END == kExpSwiglu || END == kExpSwigluKeep, OUT32 = F == kExpFp32 || END == kExpStoreFp32, MX = F == kExpMx;
     constexpr bool COLS_A = WGRAD;
+    constexpr int SLAB = (BM + BN) * kSlabBytes, SCALES = MX ? (BM + BN) * 8 : 0;
     static_assert(!GATED || TN % 2 == 0, "gate and up in one wavefront");
-    __shared__ __attribute__((aligned(128))) char s_a[BM * kSlabBytes], s_b[BN * kSlabBytes];
-    __shared__ unsigned char s_sa[MX ? BM * 8 : 1], s_sb[MX ? BN * 8 : 1];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / WN, wn = wave % WN;
+    static_assert(BM * 8 % NT == 0 && BN * 8 % NT == 0, "as many loads to every wavefront");
+    __shared__ __attribute__((aligned(1024))) char s_mem[2 * (SLAB + SCALES)];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
 
     const int per = p.mt * p.nt, j = blockIdx.x / per, t = blockIdx.x - j * per;
     const int m0 = t / p.nt * BM, n0 = t % p.nt * (GATED ? BN / 2 : BN);
@@ -189,30 +202,87 @@ __global__ __launch_bounds__(64 * WM * WN) void k_expert_product(ExpertArgs p)
             for (int e = 0; e < 16; ++e) acc[i][u][e] = 0.f;
 
     if (m0 < ms) {
-        const size_t row_a = (size_t)(WGRAD ? p.M : p.K) * 16 / CE;
+        const size_t row_a = (size_t)(WGRAD ? p.M : p.K) * 16 / CE, row_b = (size_t)(COLS_B ? n_all : p.K) * 16 / CE;     // bytes
         const char *a = (const char *)p.a + (size_t)j * p.C * row_a;
-        const char *b = (const char *)p.b + (WGRAD ? (size_t)j * p.C * p.N : (size_t)j * n_all * p.K) * 16 / CE;
-        const unsigned char *sa = MX ? p.sa + (size_t)j * p.C * (p.K / 32) : nullptr, *sb = MX ? p.sb + (size_t)j * n_all * (p.K / 32) : nullptr;
-        for (int k0 = 0; k0 < ks; k0 += KS) {
-            __syncthreads();
+        const char *b = (const char *)p.b + (WGRAD ? (size_t)j * p.C : COLS_B ? (size_t)j * p.K : (size_t)j * n_all) * row_b;
+        const int blocks = p.K / 32;
+        const unsigned char *sa = MX ? p.sa + (size_t)j * p.C * blocks : nullptr, *sb = MX ? p.sb + (size_t)j * n_all * blocks : nullptr;
+        const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)s_mem + wave * 1024;
+        constexpr int NA = BM * 8 / NT, NB = BN * 8 / NT, NSC = MX ? (BM + BN + NT - 1) / NT : 1;
+        unsigned off_a[NA], off_b[NB];
+        const char *tile_a = a + (COLS_A ? (size_t)m0 * 16 / CE : m0 * row_a), *tile_b = b + (COLS_B ? (size_t)n0 * 16 / CE : n0 * row_b);
+        const size_t next_a = COLS_A ? KS * row_a : kSlabBytes, next_b = COLS_B ? KS * row_b : kSlabBytes;
+        if constexpr (ALIGNED) {
 #pragma unroll
-            for (int q = tid; q < BM * 8; q += NT) {
+            for (int i = 0; i < NA; ++i) {
                 int row, col;
-                ex_place<F, COLS_A, BM>(q, row, col);
-                *(ex_u32x4 *)(s_a + q * 16) = COLS_A ? ex_load16<F, ALIGNED>(a, k0 + row, m0 + col, ks, p.M) : ex_load16<F, ALIGNED>(a, m0 + row, k0 + col, ms, p.K);
+                ex_place<F, COLS_A, BM>(tid + i * NT, row, col);
+                off_a[i] = COLS_A ? (unsigned)(row * row_a) + (m0 + col < p.M ? col : p.M - CE - m0) * 16 / CE
+                                  : (unsigned)((m0 + row < ms ? row : ms - 1 - m0) * row_a) + col * 16 / CE;
             }
 #pragma unroll
-            for (int q = tid; q < BN * 8; q += NT) {
+            for (int i = 0; i < NB; ++i) {
                 int row, col;
-                ex_place<F, COLS_B, BN>(q, row, col);
-                *(ex_u32x4 *)(s_b + q * 16) = COLS_B ? ex_load16<F, ALIGNED>(b, k0 + row, b_index(col), ks, n_all) : ex_load16<F, ALIGNED>(b, b_index(row), k0 + col, n_all, p.K);
+                ex_place<F, COLS_B, BN>(tid + i * NT, row, col);
+                const int c = COLS_B ? col : row, at = b_index(c), last = COLS_B ? n_all - CE : n_all - 1;
+                const unsigned d = (unsigned)((at < n_all ? at : last) - n0);
+                off_b[i] = COLS_B ? (unsigned)(row * row_b) + d * 16 / CE : (unsigned)(d * row_b) + col * 16 / CE;
+            }
+        }
+        // the scales of a slab, eight bytes to a row of the tile, on their way in registers
+        unsigned long long sc[NSC];
+        const unsigned char *row_s[NSC];
+        if constexpr (MX) {
+#pragma unroll
+            for (int i = 0; i < NSC; ++i) {
+                const int r = tid + i * NT;
+                if (r < BM) row_s[i] = sa + (size_t)(m0 + r < ms ? m0 + r : ms - 1) * blocks;
+                else row_s[i] = sb + (size_t)(r < BM + BN && b_index(r - BM) < n_all ? b_index(r - BM) : n_all - 1) * blocks;
+            }
+        }
+        auto fetch = [&](int slab, int buf) {
+            const char *pa = tile_a + slab * next_a, *pb = tile_b + slab * next_b;
+#pragma unroll
+            for (int i = 0; i < NA; ++i) ex_load_lds(pa, off_a[i], lds + buf * SLAB + i * NT * 16);
+#pragma unroll
+            for (int i = 0; i < NB; ++i) ex_load_lds(pb, off_b[i], lds + buf * SLAB + BM * kSlabBytes + i * NT * 16);
+            if constexpr (MX)
+#pragma unroll
+                for (int i = 0; i < NSC; ++i) __builtin_memcpy(&sc[i], row_s[i] + slab * 8, 8);
+        };
+        auto put_scales = [&](int buf) {
+#pragma unroll
+            for (int i = 0; i < NSC; ++i)
+                if (tid + i * NT < BM + BN) *(unsigned long long *)(s_mem + 2 * SLAB + buf * SCALES + (tid + i * NT) * 8) = sc[i];
+        };
+        auto fill = [&](int slab, int buf) {
+            char *s_a = s_mem + buf * SLAB, *s_b = s_a + BM * kSlabBytes;
+            const int k0 = slab * KS;
+#pragma unroll
+            for (int i = 0; i < NA; ++i) {
+                int row, col;
+                ex_place<F, COLS_A, BM>(tid + i * NT, row, col);
+                *(ex_u32x4 *)(s_a + (tid + i * NT) * 16) = COLS_A ? ex_load16<F, ALIGNED>(a, k0 + row, m0 + col, ks, p.M) : ex_load16<F, ALIGNED>(a, m0 + row, k0 + col, ms, p.K);
+            }
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+                int row, col;
+                ex_place<F, COLS_B, BN>(tid + i * NT, row, col);
+                *(ex_u32x4 *)(s_b + (tid + i * NT) * 16) = COLS_B ? ex_load16<F, ALIGNED>(b, k0 + row, b_index(col), ks, n_all) : ex_load16<F, ALIGNED>(b, b_index(row), k0 + col, n_all, p.K);
             }
             if constexpr (MX) {
-                const int blocks = p.K / 32, k32 = k0 / 32;
-                for (int q = tid; q < BM * 8; q += NT) s_sa[q] = m0 + (q >> 3) < ms && k32 + (q & 7) < blocks ? sa[(size_t)(m0 + (q >> 3)) * blocks + k32 + (q & 7)] : 0;
-                for (int q = tid; q < BN * 8; q += NT) s_sb[q] = b_index(q >> 3) < n_all && k32 + (q & 7) < blocks ? sb[(size_t)b_index(q >> 3) * blocks + k32 + (q & 7)] : 0;
+#pragma unroll
+                for (int i = 0; i < NSC; ++i) {
+                    sc[i] = 0;
+                    for (int e = 0; e < 8; ++e)
+                        if (slab * 8 + e < blocks) sc[i] |= (unsigned long long)row_s[i][slab * 8 + e] << (8 * e);
+                }
+                put_scales(buf);
             }
-            __syncthreads();
+        };
+        const bool busy = m0 + wm * TM * 32 < ms;           // the others have nothing but rows that the result does not have
+        auto compute = [&](int buf) {
+            const char *s_a = s_mem + buf * SLAB, *s_b = s_a + BM * kSlabBytes, *s_sa = s_mem + 2 * SLAB + buf * SCALES, *s_sb = s_sa + BM * 8;
             int va[TM], vb[TN];
 #pragma unroll
             for (int i = 0; i < TM; ++i) va[i] = MX ? *(const int *)(s_sa + (wm * TM * 32 + i * 32 + (lane & 31)) * 8 + 4 * (lane >> 5)) : 0;
@@ -234,6 +304,19 @@ __global__ __launch_bounds__(64 * WM * WN) void k_expert_product(ExpertArgs p)
             step(std::integral_constant<int, 1>{});
             step(std::integral_constant<int, 2>{});
             step(std::integral_constant<int, 3>{});
+        };
+        const int slabs = (ks + KS - 1) / KS, whole = ALIGNED ? ks / KS : 0;
+        if (whole > 0) fetch(0, 0);
+        for (int i = 0; i < slabs; ++i) {
+            if (i < whole) {
+                ex_loads_done();
+                if constexpr (MX) put_scales(i & 1);
+            } else {
+                fill(i, i & 1);
+            }
+            __syncthreads();
+            if (i + 1 < whole) fetch(i + 1, (i + 1) & 1);
+            if (busy) compute(i & 1);
         }
     }
 
@@ -271,7 +354,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_expert_product(ExpertArgs p)
     }
 }
 
-template <int F, bool COLS_B, bool WGRAD, int END, bool ALIGNED, int WM, int WN, int TM, int TN>
+template <int F, bool COLS_B, bool WGRAD, int END, bool ALIGNED, int WM, int WN, int TM, int TN, int WGS>
 int32_t ex_launch(ExpertArgs p, hipStream_t s)
 {
     constexpr bool GATED = END == kExpSwiglu || END == kExpSwigluKeep;
@@ -280,18 +363,20 @@ int32_t ex_launch(ExpertArgs p, hipStream_t s)
     p.nt = (p.N + BN - 1) / BN;
     const long long tiles = (long long)p.mt * p.nt * p.E;
     if (tiles > 0xffffffffll / (64 * WM * WN)) return MAXSCORE_ERR_SHAPE;      // a launch counts its threads in 32 bits
-    hipLaunchKernelGGL((k_expert_product<F, COLS_B, WGRAD, END, ALIGNED, WM, WN, TM, TN>), dim3((unsigned)tiles), dim3(64 * WM * WN), 0, s, p);
+    hipLaunchKernelGGL((k_expert_product<F, COLS_B, WGRAD, END, ALIGNED, WM, WN, TM, TN, WGS>), dim3((unsigned)tiles), dim3(64 * WM * WN), 0, s, p);
     MS_HIP(hipGetLastError());
     return MAXSCORE_OK;
 }
 
-// Whether all rows of the operands and the results begin on 16 bytes and are whole numbers of them.
+// Whether all rows of the operands and the results begin on 16 bytes and are whole numbers of them, and a tile's offsets fit 32 bits (gate and up rows
+// are N apart).
 template <int F>
-bool ex_aligned(const ExpertArgs &p, bool cols_b, bool wgrad)
+bool ex_aligned(const ExpertArgs &p, bool cols_b, bool wgrad, bool gated)
 {
     constexpr int CE = ExpertElem<F>::chunk;
     const uintptr_t at = (uintptr_t)p.a | (uintptr_t)p.b | (uintptr_t)p.out | (uintptr_t)p.keep;
     if (at % 16 || p.N % (F == kExpMx ? 8 : CE)) return false;
+    if (gated && !cols_b && ((long long)p.N + 256) * p.K * 16 / CE >> 32) return false;
     return wgrad ? p.M % CE == 0 : p.K % CE == 0;
 }
 
