@@ -5,13 +5,16 @@
 // An operand is "rows" (k contiguous in memory: x[rows, K], W[E, N, K]) or "cols" (k is the row index: W[E, K, N]; both operands of the
 // weight gradient, where k counts the expert's rows).  k is walked in slabs of 128 bytes of an operand's row: 64 bf16, 32 fp32, 256 four-bit
 // numbers.  A slab of R rows takes R * 128 bytes of LDS either way, in 16-byte chunks:
-//   rows  row r, chunk c at r * 128 + 16 * (c ^ (r & 7)): eight rows' chunks of one column lie in eight different places of 128 bytes
+//   rows  row r, chunk c at r * 128 + 16 * (c ^ (r / 2 & 7)): a column's chunks of sixteen rows lie in the sixteen places of 256 bytes, which are
+//         read at a time (turned by r & 7, two rows to a place, 64 x 2048 rows of 2048 to 1024 took 571 us, 556 so)
 //   cols  k's row of R elements, chunk c at k * R * size + 16 * (c ^ turn(k)), where turn spreads four rows over 256 bytes
 // and is read in the layout of 32x32 matrix instructions: lane l has row l % 32 of a block and chunk 4 * (l / 32) + kk of the slab in step kk.
 // Which of the slab's k a lane has in a step does not matter as long as both operands agree.  Operands that are cols come through LDS's
 // transposing reads (bf16: four k of sixteen rows at a time) or word by word (fp32, whose matrix instructions take eight times as long).
 // B is the instruction's first operand, so that a lane ends with four neighbouring columns n of one row m.
 #pragma once
+#include <algorithm>
+
 #include "expert_steps.h"
 
 namespace maxscore {
@@ -27,6 +30,7 @@ typedef __attribute__((ext_vector_type(4))) float ex_f32x4;
 typedef __attribute__((ext_vector_type(8))) int ex_i32x8;
 
 constexpr int kSlabBytes = 128;
+constexpr int kTilesTogether = 32;      // what a die has compute units
 
 // Elements of a format to 16 bytes, and bits of one.
 template <int F> struct ExpertElem;
@@ -87,7 +91,7 @@ __device__ __forceinline__ void ex_place(int q, int &row, int &col)
     constexpr int CE = ExpertElem<F>::chunk;
     if constexpr (!COLS) {
         row = q >> 3;
-        col = ((q & 7) ^ (row & 7)) * CE;
+        col = ((q & 7) ^ (row >> 1 & 7)) * CE;
     } else {
         constexpr int CPR = R / CE;
         row = q / CPR;
@@ -108,7 +112,7 @@ __device__ __forceinline__ ExpertFrag<F> ex_fragment(const char *slab, int rb, i
     const int c = 4 * (lane >> 5) + kk;
     if constexpr (!COLS) {
         const int r = rb * 32 + (lane & 31);
-        const ex_u32x4 v = *(const ex_u32x4 *)(slab + r * kSlabBytes + ((c ^ (r & 7)) << 4));
+        const ex_u32x4 v = *(const ex_u32x4 *)(slab + r * kSlabBytes + ((c ^ (r >> 1 & 7)) << 4));
         f.v = __builtin_bit_cast(decltype(f.v), v);
     } else if constexpr (F == kExpBf16) {
         typedef __attribute__((address_space(3))) ex_bf16x4 *lds_quad;
@@ -144,25 +148,55 @@ __device__ __forceinline__ ex_f32x16 ex_mma(const ExpertFrag<F> &b, const Expert
 // u * g / (1 + e^-g).  Where e^-g is infinite the quotient is zero, as it should be.
 __device__ __forceinline__ float ex_silu_times(float g, float u) { return u * (g / (1.f + expf(-g))); }
 
-// Four neighbouring columns of a row of the result, in the type of the result.
-template <bool FP32, bool ALIGNED>
-__device__ __forceinline__ void ex_store4(void *out, size_t at, int left, const float (&v)[4])
+// Four neighbouring values as they lie in memory, in fp32 or rounded to bf16.
+template <bool FP32>
+__device__ __forceinline__ auto ex_pack4(const float (&v)[4])
 {
-    if constexpr (FP32) {
-        float *p = (float *)out + at;
-        if (ALIGNED) *(ex_f32x4 *)p = ex_f32x4{v[0], v[1], v[2], v[3]};
-        else
+    if constexpr (FP32) return ex_f32x4{v[0], v[1], v[2], v[3]};
+    else return ex_u32x2{ex_to_bf16(v[0]) | (unsigned)ex_to_bf16(v[1]) << 16, ex_to_bf16(v[2]) | (unsigned)ex_to_bf16(v[3]) << 16};
+}
+
+// A wavefront's 32 rows of COLS columns of the result at row m, column n of `out`, rows of PITCH * cols of which `cols` are its.  A lane has four columns of one row at a time
+// (values(q, v): columns 8 q + 4 (lane / 32) .. of row lane % 32), which would be 32 stores to as many lines; through its part of LDS (chunks turned as in a slab) they
+// become whole lines.  Rows that are no whole numbers of 16 bytes are stored value by value.
+template <bool FP32, bool ALIGNED, int COLS, int PITCH = 1, typename V>
+__device__ __forceinline__ void ex_put_rows(char *scratch, void *out, int m, int n, int rows, int cols, int lane, V values)
+{
+    constexpr int SIZE = FP32 ? 4 : 2, CPR = COLS * SIZE / 16, PER = 16 / SIZE, ALL = 32 * CPR;
+    if constexpr (ALIGNED) {
+        constexpr int TURN = CPR < 8 ? CPR : 8;
+        const int r = lane & 31;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (i < left) p[i] = v[i];
+        for (int q = 0; q < COLS / 8; ++q) {
+            float v[4];
+            values(q, v);
+            const int at = (8 * q + 4 * (lane >> 5)) * SIZE;
+            *(decltype(ex_pack4<FP32>(v)) *)(scratch + r * (CPR * 16) + (((at >> 4) ^ (r >> 1 & (TURN - 1))) << 4) + (at & 15)) = ex_pack4<FP32>(v);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // the lanes exchange: LDS goes in order, the compiler has to as well
+#pragma unroll
+        for (int i = 0; i < ALL; i += 64) {
+            const int row = (i + lane) / CPR, c = (i + lane) % CPR;
+            if (ALL % 64 && i + lane >= ALL) break;
+            const ex_u32x4 x = *(const ex_u32x4 *)(scratch + row * (CPR * 16) + ((c ^ (row >> 1 & (TURN - 1))) << 4));
+            if (m + row < rows && n + c * PER < cols) *(ex_u32x4 *)((char *)out + ((size_t)(m + row) * (PITCH * (size_t)cols) + n + c * PER) * SIZE) = x;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     } else {
-        unsigned short *p = (unsigned short *)out + at;
-        if (ALIGNED)
-            *(ex_u32x2 *)p = ex_u32x2{ex_to_bf16(v[0]) | (unsigned)ex_to_bf16(v[1]) << 16, ex_to_bf16(v[2]) | (unsigned)ex_to_bf16(v[3]) << 16};
-        else
+        if (m + (lane & 31) >= rows) return;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (i < left) p[i] = ex_to_bf16(v[i]);
+        for (int q = 0; q < COLS / 8; ++q) {
+            float v[4];
+            values(q, v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int c = n + 8 * q + 4 * (lane >> 5) + e;
+                const size_t at = (size_t)(m + (lane & 31)) * (PITCH * (size_t)cols) + c;
+                if (c >= cols) continue;
+                if constexpr (FP32) ((float *)out)[at] = v[e];
+                else ((unsigned short *)out)[at] = ex_to_bf16(v[e]);
+            }
+        }
     }
 }
 
@@ -184,7 +218,11 @@ __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_prod
     __shared__ __attribute__((aligned(1024))) char s_mem[2 * (SLAB + SCALES)];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
 
-    const int per = p.mt * p.nt, j = blockIdx.x / per, t = blockIdx.x - j * per;
+    // Workgroups go to the eight dies in turn; a die takes `together` neighbouring tiles, whose operands meet in its L2.
+    const unsigned die = blockIdx.x & 7u, turn = blockIdx.x >> 3;
+    const unsigned tile = (turn / p.together * 8 + die) * p.together + turn % p.together;
+    const int per = p.mt * p.nt, j = tile / per, t = tile - j * per;
+    if (j >= p.E) return;
     const int m0 = t / p.nt * BM, n0 = t % p.nt * (GATED ? BN / 2 : BN);
     const int o0 = p.offsets[j], cnt = p.offsets[j + 1] - o0, filled = cnt < 0 ? 0 : cnt < p.C ? cnt : p.C;
     const int ms = WGRAD ? p.M : filled, ks = WGRAD ? filled : p.K;           // rows of the result that have sums, length of these
@@ -321,36 +359,37 @@ __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_prod
     }
 
     // rows of the buffer that hold nothing are zero
-    const size_t out0 = (size_t)j * p.M * p.N, keep0 = (size_t)j * p.M * n_all;
+    constexpr int SIZE = OUT32 ? 4 : 2, COLS = GATED ? TN * 16 : TN * 32;
+    static_assert(WM * WN * 32 * COLS * SIZE <= sizeof(s_mem), "every wavefront's part");
+    char *scratch = s_mem + wave * (32 * COLS * SIZE), *out = (char *)p.out + (size_t)j * p.M * p.N * SIZE;
+    if (ALIGNED) __syncthreads();
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-        const int m = m0 + (wm * TM + i) * 32 + (lane & 31);
-        if (m >= p.M) continue;
-        const bool has = m < ms;
+        const int m = m0 + (wm * TM + i) * 32, n = n0 + wn * COLS;
+        if (m >= p.M) break;
+        const bool has = m + (lane & 31) < ms;
+        auto sums = [&](int u, int q, float(&v)[4]) {
 #pragma unroll
-        for (int u = 0; u < TN; u += GATED ? 2 : 1)
+            for (int e = 0; e < 4; ++e) v[e] = has ? acc[i][u][4 * q + e] : 0.f;
+        };
+        if constexpr (GATED) {
+            ex_put_rows<OUT32, ALIGNED, COLS>(scratch, out, m, n, p.M, p.N, lane, [&](int q, float(&v)[4]) {
+                float w[4];
+                sums(q / 4 * 2, q % 4, v);
+                sums(q / 4 * 2 + 1, q % 4, w);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int n = n0 + (GATED ? (wn * TN + u) * 16 : (wn * TN + u) * 32) + 8 * q + 4 * (lane >> 5), left = p.N - n;
-                if (left <= 0) continue;
-                float v[4];
+                for (int e = 0; e < 4; ++e) v[e] = ex_silu_times(v[e], w[e]);
+            });
+            if constexpr (END == kExpSwigluKeep) {
+                // rows of gate and up are one row of 2 N: gate's columns end at N
+                char *keep = (char *)p.keep + (size_t)j * p.M * n_all * SIZE;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = has ? acc[i][u][4 * q + e] : 0.f;
-                if constexpr (GATED) {
-                    float w[4], h[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] = has ? acc[i][u + 1][4 * q + e] : 0.f;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) h[e] = ex_silu_times(v[e], w[e]);
-                    ex_store4<OUT32, ALIGNED>(p.out, out0 + (size_t)m * p.N + n, left, h);
-                    if constexpr (END == kExpSwigluKeep) {
-                        ex_store4<OUT32, ALIGNED>(p.keep, keep0 + (size_t)m * n_all + n, left, v);
-                        ex_store4<OUT32, ALIGNED>(p.keep, keep0 + (size_t)m * n_all + p.N + n, left, w);
-                    }
-                } else {
-                    ex_store4<OUT32, ALIGNED>(p.out, out0 + (size_t)m * p.N + n, left, v);
-                }
+                for (int half = 0; half < 2; ++half)
+                    ex_put_rows<OUT32, ALIGNED, COLS, 2>(scratch, keep + (size_t)half * p.N * SIZE, m, n, p.M, p.N, lane, [&](int q, float(&v)[4]) { sums(q / 4 * 2 + half, q % 4, v); });
             }
+        } else {
+            ex_put_rows<OUT32, ALIGNED, COLS>(scratch, out, m, n, p.M, p.N, lane, [&](int q, float(&v)[4]) { sums(q / 4, q % 4, v); });
+        }
     }
 }
 
@@ -361,7 +400,9 @@ int32_t ex_launch(ExpertArgs p, hipStream_t s)
     constexpr int BM = 32 * WM * TM, BN = 32 * WN * TN / (GATED ? 2 : 1);
     p.mt = (p.M + BM - 1) / BM;
     p.nt = (p.N + BN - 1) / BN;
-    const long long tiles = (long long)p.mt * p.nt * p.E;
+    const long long real = (long long)p.mt * p.nt * p.E;
+    p.together = (int)std::min<long long>(kTilesTogether, (real + 7) / 8);          // few tiles: an equal share to every die
+    const long long all = 8 * p.together, tiles = (real + all - 1) / all * all;
     if (tiles > 0xffffffffll / (64 * WM * WN)) return MAXSCORE_ERR_SHAPE;      // a launch counts its threads in 32 bits
     hipLaunchKernelGGL((k_expert_product<F, COLS_B, WGRAD, END, ALIGNED, WM, WN, TM, TN, WGS>), dim3((unsigned)tiles), dim3(64 * WM * WN), 0, s, p);
     MS_HIP(hipGetLastError());
