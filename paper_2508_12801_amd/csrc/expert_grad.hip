@@ -7,6 +7,9 @@
 namespace maxscore {
 namespace {
 
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
 template <typename T> __device__ __forceinline__ float to_f32(T v);
 template <> __device__ __forceinline__ float to_f32<unsigned short>(unsigned short v) { return __uint_as_float((unsigned)v << 16); }
 template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
@@ -45,21 +48,135 @@ __global__ __launch_bounds__(256) void k_swiglu_backward(const T *__restrict__ g
     }
 }
 
-// One wavefront per token and its slots; the workgroups behind them zero the places that hold nothing.
-template <typename T>
+// The sum over the wavefront's lanes, as a tree: within sixteen lanes by lane moves, the four rows' sums one by one.
+template <int CTRL>
+__device__ __forceinline__ float add_lane(float v)
+{
+    return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float wave_sum(float v)
+{
+    v = add_lane<0xb1>(v);       // quads
+    v = add_lane<0x4e>(v);
+    v = add_lane<0x141>(v);      // halves of a row mirrored, then the row
+    v = add_lane<0x140>(v);
+    const int w = __float_as_int(v);
+    return (__int_as_float(__builtin_amdgcn_readlane(w, 0)) + __int_as_float(__builtin_amdgcn_readlane(w, 16))) +
+           (__int_as_float(__builtin_amdgcn_readlane(w, 32)) + __int_as_float(__builtin_amdgcn_readlane(w, 48)));
+}
+
+// A wavefront takes a token, or `parts` of them share its slots where there are few tokens.  It has HOLD * 64 pieces of 16 bytes of a row of the buffers in
+// its registers at a time (a piece: eight columns of bf16, four of fp32), the token's dy once for all its slots, which go two at a time so that one's
+// rows are on their way while the other's are used.  Lane s keeps slot s's gate and sum.  Bound by HBM: dy once, rows in, rows out.
+// The workgroups from n_wg on zero the places that hold nothing, an equal share of every expert's.
+template <typename T, int HOLD, bool NT>
 __global__ __launch_bounds__(256) void k_combine_backward(const float *__restrict__ dy, const T *__restrict__ expert_out,
                                                           const int32_t *__restrict__ assign, const int32_t *__restrict__ token_pos,
                                                           const float *__restrict__ gates, const int32_t *__restrict__ offsets, int T_, int d, int E,
-                                                          int k, int C, int n_wg, T *__restrict__ dexpert_out, float *__restrict__ dgates)
+                                                          int k, int C, int parts, int n_wg, int shares, T *__restrict__ dexpert_out,
+                                                          float *__restrict__ dgates)
+{
+    constexpr int PER = 16 / sizeof(T);
+    const int lane = threadIdx.x & 63, pieces = d / PER;
+    if ((int)blockIdx.x >= n_wg) {
+        const int j = (blockIdx.x - n_wg) / shares, share = (blockIdx.x - n_wg) % shares;
+        const int n = filled_rows(offsets, j, C);
+        const size_t all = (size_t)(C - n) * pieces, from = all * share / shares, to = all * (share + 1) / shares;
+        u32x4 *p = (u32x4 *)(dexpert_out + ((size_t)j * C + n) * d);
+        for (size_t i = from + threadIdx.x; i < to; i += 256) p[i] = u32x4{0u, 0u, 0u, 0u};
+        return;
+    }
+    const unsigned item = blockIdx.x * 4u + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = item / (unsigned)parts, part = item % (unsigned)parts;
+    if (i >= (unsigned)T_) return;
+    const int s0 = (int)((long long)k * part / parts), s1 = (int)((long long)k * (part + 1) / parts);
+    int expert = -1, row = 0;
+    float gate = 0.f, sum = 0.f;
+    if (lane >= s0 && lane < s1) {
+        const size_t at = (size_t)i * k + lane;
+        expert = assign[at];
+        row = token_pos[at];
+        gate = gates[at];
+        if (expert >= E || row < 0 || row >= C) expert = -1;       // an empty slot, or a place outside the buffer
+    }
+    const f32x4 *dyr = (const f32x4 *)(dy + (size_t)i * d);
+    for (int c0 = 0; c0 < pieces; c0 += 64 * HOLD) {
+        f32x4 g[HOLD][PER / 4];
+#pragma unroll
+        for (int u = 0; u < HOLD; ++u) {
+            const int c = c0 + 64 * u + lane;
+#pragma unroll
+            for (int w = 0; w < PER / 4; ++w) g[u][w] = c < pieces ? dyr[(size_t)c * (PER / 4) + w] : f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        auto fetch = [&](int s, u32x4(&v)[HOLD]) {
+            const int e = __builtin_amdgcn_readlane(expert, s);
+            if (e < 0) return;
+            const u32x4 *src = (const u32x4 *)expert_out + ((size_t)e * C + __builtin_amdgcn_readlane(row, s)) * pieces;
+#pragma unroll
+            for (int u = 0; u < HOLD; ++u) {
+                const int c = c0 + 64 * u + lane;
+                v[u] = NT ? __builtin_nontemporal_load(src + (c < pieces ? c : pieces - 1)) : src[c < pieces ? c : pieces - 1];
+            }
+        };
+        auto use = [&](int s, const u32x4(&v)[HOLD]) {
+            const int e = __builtin_amdgcn_readlane(expert, s);
+            if (e < 0) return;
+            const float gs = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(gate), s));
+            u32x4 *dst = (u32x4 *)dexpert_out + ((size_t)e * C + __builtin_amdgcn_readlane(row, s)) * pieces;
+            float dot = 0.f;
+#pragma unroll
+            for (int u = 0; u < HOLD; ++u) {
+                const int c = c0 + 64 * u + lane;
+                u32x4 out;
+                if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const float a = g[u][w / 2][w % 2 * 2], b = g[u][w / 2][w % 2 * 2 + 1];
+                        if (c < pieces) {
+                            dot = fmaf(a, __uint_as_float(v[u][w] << 16), dot);
+                            dot = fmaf(b, __uint_as_float(v[u][w] & 0xffff0000u), dot);
+                        }
+                        out[w] = from_f32<unsigned short>(gs * a) | (unsigned)from_f32<unsigned short>(gs * b) << 16;
+                    }
+                } else {
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        if (c < pieces) dot = fmaf(g[u][0][w], __uint_as_float(v[u][w]), dot);
+                        out[w] = __float_as_uint(gs * g[u][0][w]);
+                    }
+                }
+                if (c < pieces) {
+                    if (NT) __builtin_nontemporal_store(out, dst + c);
+                    else dst[c] = out;
+                }
+            }
+            dot = wave_sum(dot);
+            if (lane == s) sum += dot;
+        };
+        u32x4 v0[HOLD], v1[HOLD];
+        fetch(s0, v0);
+        for (int s = s0; s < s1; s += 2) {
+            if (s + 1 < s1) fetch(s + 1, v1);
+            use(s, v0);
+            if (s + 2 < s1) fetch(s + 2, v0);
+            if (s + 1 < s1) use(s + 1, v1);
+        }
+    }
+    if (lane >= s0 && lane < s1) dgates[(size_t)i * k + lane] = sum;
+}
+
+// Rows that are no whole numbers of 16 bytes, or do not begin on them: value by value.
+template <typename T>
+__global__ __launch_bounds__(256) void k_combine_backward_elem(const float *__restrict__ dy, const T *__restrict__ expert_out,
+                                                               const int32_t *__restrict__ assign, const int32_t *__restrict__ token_pos,
+                                                               const float *__restrict__ gates, const int32_t *__restrict__ offsets, int T_, int d,
+                                                               int E, int k, int C, int n_wg, T *__restrict__ dexpert_out, float *__restrict__ dgates)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if ((int)blockIdx.x >= n_wg) {
-        for (int j = blockIdx.x - n_wg; j < E; j += gridDim.x - n_wg) {
-            const int n = filled_rows(offsets, j, C);
-            T *p = dexpert_out + ((size_t)j * C + n) * d;
-            const size_t all = (size_t)(C - n) * d;
-            for (size_t i = threadIdx.x; i < all; i += 256) p[i] = (T)0;
-        }
+        const int j = blockIdx.x - n_wg, n = filled_rows(offsets, j, C);
+        T *p = dexpert_out + ((size_t)j * C + n) * d;
+        const size_t all = (size_t)(C - n) * d;
+        for (size_t i = threadIdx.x; i < all; i += 256) p[i] = (T)0;
         return;
     }
     const int i = blockIdx.x * 4 + wave;
@@ -76,7 +193,7 @@ __global__ __launch_bounds__(256) void k_combine_backward(const float *__restric
                 sum = fmaf(v, to_f32(expert_out[row + c]), sum);
                 dexpert_out[row + c] = from_f32<T>(g * v);
             }
-            for (int w = 32; w; w >>= 1) sum += __shfl_xor(sum, w);
+            sum = wave_sum(sum);
         }
         if (lane == 0) dgates[at] = sum;
     }
@@ -101,13 +218,30 @@ int32_t swiglu_backward_run(const void *gate_up, const void *dh, int dtype, cons
 int32_t combine_backward_run(const float *dy, const void *expert_out, int dtype, const int32_t *assign, const int32_t *token_pos, const float *gates,
                              const int32_t *offsets, int T, int d, int E, int k, int C, void *dexpert_out, float *dgates, hipStream_t s)
 {
-    const int n_wg = (T + 3) / 4;
-    if (dtype == MAXSCORE_DTYPE_BF16)
-        hipLaunchKernelGGL((k_combine_backward<unsigned short>), dim3(n_wg + E), dim3(256), 0, s, dy, (const unsigned short *)expert_out, assign, token_pos,
-                           gates, offsets, T, d, E, k, C, n_wg, (unsigned short *)dexpert_out, dgates);
-    else
-        hipLaunchKernelGGL((k_combine_backward<float>), dim3(n_wg + E), dim3(256), 0, s, dy, (const float *)expert_out, assign, token_pos, gates, offsets,
-                           T, d, E, k, C, n_wg, (float *)dexpert_out, dgates);
+    const int size = dtype == MAXSCORE_DTYPE_BF16 ? 2 : 4;
+    const bool vec = (size_t)d * size % 16 == 0 && (((uintptr_t)dy | (uintptr_t)expert_out | (uintptr_t)dexpert_out) % 16) == 0;
+    if (!vec) {
+        const int n_wg = (T + 3) / 4;
+#define MS_COMBINE_B(TT)                                                                                                                          \
+    hipLaunchKernelGGL((k_combine_backward_elem<TT>), dim3(n_wg + E), dim3(256), 0, s, dy, (const TT *)expert_out, assign, token_pos, gates, offsets, \
+                       T, d, E, k, C, n_wg, (TT *)dexpert_out, dgates)
+        if (size == 2) MS_COMBINE_B(unsigned short);
+        else MS_COMBINE_B(float);
+#undef MS_COMBINE_B
+    } else {
+        // sixteen wavefronts to a compute unit, as far as there are slots
+        const int parts = std::max(1, std::min(k, (4096 + T - 1) / T));
+        const int n_wg = (int)(((long long)T * parts + 3) / 4), shares = std::max(1, 1024 / E);
+        const bool nt = (size_t)E * C * d * size >= (size_t)256 << 20;          // beyond the last cache
+#define MS_COMBINE_B(TT, NN)                                                                                                                  \
+    hipLaunchKernelGGL((k_combine_backward<TT, 4, NN>), dim3(n_wg + E * shares), dim3(256), 0, s, dy, (const TT *)expert_out, assign, token_pos, gates, \
+                       offsets, T, d, E, k, C, parts, n_wg, shares, (TT *)dexpert_out, dgates)
+        if (size == 2 && nt) MS_COMBINE_B(unsigned short, true);
+        else if (size == 2) MS_COMBINE_B(unsigned short, false);
+        else if (nt) MS_COMBINE_B(float, true);
+        else MS_COMBINE_B(float, false);
+#undef MS_COMBINE_B
+    }
     MS_HIP(hipGetLastError());
     return MAXSCORE_OK;
 }
