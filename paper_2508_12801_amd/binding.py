@@ -569,26 +569,29 @@ def combine(expert_out, assign, token_pos, gate, out=None):
     return out
 
 
-def _operand(t, name, shape=None, dtype=None, like=None):
-    """A call's operand as the kernels take it: on the current device, packed, of the shape and type that the call's other operands ask for."""
-    torch = _torch()
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+def _here():
+    """The current device's index."""
+    return _torch().cuda.current_device()
+
+
+def _operand(t, name, here, shape=None, dtype=None):
+    """An operand's address, if it is as the kernels take it: on the current device, packed, of the shape and type that the call's others ask for."""
+    if t.get_device() != here:
         raise MaxScoreError(ERR_SHAPE, f"{name}: not on the current device")
     if not t.is_contiguous():
         raise MaxScoreError(ERR_SHAPE, f"{name}: not contiguous")
     if shape is not None and t.shape != shape:
         raise MaxScoreError(ERR_SHAPE, f"{name}: {tuple(t.shape)} instead of {tuple(shape)}")
-    want = dtype if like is None else like.dtype
-    if want is not None and t.dtype != want:
-        raise MaxScoreError(ERR_DTYPE, f"{name}: {t.dtype} instead of {want}")
+    if dtype is not None and t.dtype != dtype:
+        raise MaxScoreError(ERR_DTYPE, f"{name}: {t.dtype} instead of {dtype}")
     return t.data_ptr()
 
 
-def _result(out, name, shape, dtype, device):
+def _result(out, name, here, shape, dtype, device):
     """The caller's buffer for a result, checked, or a new one."""
     if out is None:
-        return _torch().empty(shape, dtype=dtype, device=device)
-    _operand(out, name, shape, dtype)
+        return _TORCH.empty(shape, dtype=dtype, device=device)
+    _operand(out, name, here, shape, dtype)
     return out
 
 
@@ -598,19 +601,20 @@ def _buffer(x, name, dims=3):
     return x.shape
 
 
-def _offsets_of(expert_offsets, E):
-    return _operand(expert_offsets, "expert_offsets", (E + 1,), _torch().int32)
+def _offsets_of(expert_offsets, here, E):
+    return _operand(expert_offsets, "expert_offsets", here, (E + 1,), _TORCH.int32)
 
 
 def expert_matmul(x, w, expert_offsets, transposed: bool = False, out=None):
     """y [E, C, N]: every expert's rows of x [E, C, K] (bf16 or fp32) times its w [E, K, N] (transposed: [E, N, K]).  Places beyond an expert's
     rows are not used and come back as zero.  The gradient with respect to x: the same on dy with the other `transposed`."""
+    here = _here()
     E, C, K = _buffer(x, "x")
     code = _dtype_code(x)
     N = _buffer(w, "w")[1 if transposed else 2]
-    ptrs = (_operand(x, "x"), _operand(w, "w", (E, N, K) if transposed else (E, K, N), like=x))
-    off = _offsets_of(expert_offsets, E)
-    y = _result(out, "out", (E, C, N), x.dtype, x.device)
+    ptrs = (_operand(x, "x", here), _operand(w, "w", here, (E, N, K) if transposed else (E, K, N), x.dtype))
+    off = _offsets_of(expert_offsets, here, E)
+    y = _result(out, "out", here, (E, C, N), x.dtype, x.device)
     _check(load_library().maxscore_expert_matmul(*ptrs, code, int(transposed), off, E, C, K, N, _ptr(y), _stream()), "maxscore_expert_matmul")
     return y
 
@@ -618,14 +622,15 @@ def expert_matmul(x, w, expert_offsets, transposed: bool = False, out=None):
 def expert_matmul_wgrad(x, dy, expert_offsets, dtype=None, out=None):
     """dw [E, K, N] (fp32, or `dtype` bf16 for bf16 inputs): sums over every expert's rows of x [E, C, K] and dy [E, C, N].  For transposed weights
     [E, N, K]: with x and dy exchanged."""
-    torch = _torch()
+    here = _here()
+    torch = _TORCH
     E, C, K = _buffer(x, "x")
     code = _dtype_code(x)
     N = _buffer(dy, "dy")[2]
-    ptrs = (_operand(x, "x"), _operand(dy, "dy", (E, C, N), like=x))
-    off = _offsets_of(expert_offsets, E)
+    ptrs = (_operand(x, "x", here), _operand(dy, "dy", here, (E, C, N), x.dtype))
+    off = _offsets_of(expert_offsets, here, E)
     dtype = dtype if dtype is not None else out.dtype if out is not None else torch.float32
-    dw = _result(out, "out", (E, K, N), dtype, x.device)
+    dw = _result(out, "out", here, (E, K, N), dtype, x.device)
     _check(load_library().maxscore_expert_matmul_wgrad(*ptrs, code, off, E, C, K, N, _dtype_code(dw), _ptr(dw), _stream()),
            "maxscore_expert_matmul_wgrad")
     return dw
@@ -634,16 +639,17 @@ def expert_matmul_wgrad(x, dy, expert_offsets, dtype=None, out=None):
 def expert_swiglu(x, w, expert_offsets, transposed: bool = False, want_gate_up: bool = False, out: Optional[dict] = None):
     """The experts' gated unit: dict(h [E, C, N], gate_up [E, C, 2N] or None) with [g | u] = x . w and h = u * g / (1 + e^-g); w is [E, K, 2N]
     (transposed: [E, 2N, K]), gate columns first.  gate_up is what the backward pass needs."""
+    here = _here()
     E, C, K = _buffer(x, "x")
     code = _dtype_code(x)
     N2 = _buffer(w, "w")[1 if transposed else 2]
     if N2 % 2:
         raise MaxScoreError(ERR_SHAPE, "w: as many gate as up columns expected")
-    ptrs = (_operand(x, "x"), _operand(w, "w", (E, N2, K) if transposed else (E, K, N2), like=x))
-    off = _offsets_of(expert_offsets, E)
+    ptrs = (_operand(x, "x", here), _operand(w, "w", here, (E, N2, K) if transposed else (E, K, N2), x.dtype))
+    off = _offsets_of(expert_offsets, here, E)
     out = out or {}
-    h = _result(out.get("h"), "out['h']", (E, C, N2 // 2), x.dtype, x.device)
-    gate_up = _result(out.get("gate_up"), "out['gate_up']", (E, C, N2), x.dtype, x.device) if want_gate_up else None
+    h = _result(out.get("h"), "out['h']", here, (E, C, N2 // 2), x.dtype, x.device)
+    gate_up = _result(out.get("gate_up"), "out['gate_up']", here, (E, C, N2), x.dtype, x.device) if want_gate_up else None
     rc = load_library().maxscore_expert_swiglu(*ptrs, code, int(transposed), off, E, C, K, N2 // 2, _ptr(h), _ptr(gate_up), _stream())
     _check(rc, "maxscore_expert_swiglu")
     return dict(h=h, gate_up=gate_up)
@@ -651,13 +657,14 @@ def expert_swiglu(x, w, expert_offsets, transposed: bool = False, want_gate_up: 
 
 def expert_swiglu_backward(gate_up, dh, expert_offsets, want_h: bool = True, out: Optional[dict] = None):
     """dict(dgate_up [E, C, 2N], h [E, C, N] or None) from gate_up [E, C, 2N] and dh [E, C, N]; h is the gated unit's result made again."""
+    here = _here()
     E, C, N = _buffer(dh, "dh")
     code = _dtype_code(dh)
-    ptrs = (_operand(gate_up, "gate_up", (E, C, 2 * N), like=dh), _operand(dh, "dh"))
-    off = _offsets_of(expert_offsets, E)
+    ptrs = (_operand(gate_up, "gate_up", here, (E, C, 2 * N), dh.dtype), _operand(dh, "dh", here))
+    off = _offsets_of(expert_offsets, here, E)
     out = out or {}
-    dgate_up = _result(out.get("dgate_up"), "out['dgate_up']", (E, C, 2 * N), dh.dtype, dh.device)
-    h = _result(out.get("h"), "out['h']", (E, C, N), dh.dtype, dh.device) if want_h else None
+    dgate_up = _result(out.get("dgate_up"), "out['dgate_up']", here, (E, C, 2 * N), dh.dtype, dh.device)
+    h = _result(out.get("h"), "out['h']", here, (E, C, N), dh.dtype, dh.device) if want_h else None
     rc = load_library().maxscore_expert_swiglu_backward(*ptrs, code, off, E, C, N, _ptr(dgate_up), _ptr(h), _stream())
     _check(rc, "maxscore_expert_swiglu_backward")
     return dict(dgate_up=dgate_up, h=h)
@@ -666,16 +673,17 @@ def expert_swiglu_backward(gate_up, dh, expert_offsets, want_h: bool = True, out
 def combine_backward(dy, expert_out, assign, token_pos, gate, expert_offsets, out: Optional[dict] = None):
     """The gradients of combine: dict(dexpert_out [E, C, d] in expert_out's type, dgates [T, k] fp32) from dy [T, d] fp32.  (The gradient of
     dispatch_tokens with respect to x is combine of the buffers' gradient with gates of 1.)"""
-    torch = _torch()
+    here = _here()
+    torch = _TORCH
     E, C, d = _buffer(expert_out, "expert_out")
     code = _dtype_code(expert_out)
     T, k = _buffer(assign, "assign", 2)
-    ptrs = (_operand(dy, "dy", (T, d), torch.float32), _operand(expert_out, "expert_out"))
-    lists = (_operand(assign, "assign", None, torch.int32), _operand(token_pos, "token_pos", (T, k), torch.int32),
-             _operand(gate, "gate", (T, k), torch.float32), _offsets_of(expert_offsets, E))
+    ptrs = (_operand(dy, "dy", here, (T, d), torch.float32), _operand(expert_out, "expert_out", here))
+    lists = (_operand(assign, "assign", here, None, torch.int32), _operand(token_pos, "token_pos", here, (T, k), torch.int32),
+             _operand(gate, "gate", here, (T, k), torch.float32), _offsets_of(expert_offsets, here, E))
     out = out or {}
-    dexpert_out = _result(out.get("dexpert_out"), "out['dexpert_out']", (E, C, d), expert_out.dtype, expert_out.device)
-    dgates = _result(out.get("dgates"), "out['dgates']", (T, k), torch.float32, expert_out.device)
+    dexpert_out = _result(out.get("dexpert_out"), "out['dexpert_out']", here, (E, C, d), expert_out.dtype, expert_out.device)
+    dgates = _result(out.get("dgates"), "out['dgates']", here, (T, k), torch.float32, expert_out.device)
     rc = load_library().maxscore_combine_backward(*ptrs, code, *lists, T, d, E, k, C, _ptr(dexpert_out), _ptr(dgates), _stream())
     _check(rc, "maxscore_combine_backward")
     return dict(dexpert_out=dexpert_out, dgates=dgates)
@@ -684,40 +692,43 @@ def combine_backward(dy, expert_out, assign, token_pos, gate, expert_offsets, ou
 def mxfp4_quantise(x, out=None):
     """(q uint8 [..., d/2], scales uint8 [..., d/32]) of x [..., d] (bf16 or fp32), d a multiple of 32: blocks of 32 four-bit numbers with a
     power of two each.  out: a pair of tensors to use."""
-    torch = _torch()
+    here = _here()
+    torch = _TORCH
     code = _dtype_code(x)
     if x.dim() < 1 or x.shape[-1] % 32 or x.numel() == 0:
         raise MaxScoreError(ERR_SHAPE, "x: rows of a multiple of 32 values expected")
     d = x.shape[-1]
-    ptr = _operand(x, "x")
-    q = _result(out[0] if out is not None else None, "out[0]", (*x.shape[:-1], d // 2), torch.uint8, x.device)
-    scales = _result(out[1] if out is not None else None, "out[1]", (*x.shape[:-1], d // 32), torch.uint8, x.device)
+    ptr = _operand(x, "x", here)
+    q = _result(out[0] if out is not None else None, "out[0]", here, (*x.shape[:-1], d // 2), torch.uint8, x.device)
+    scales = _result(out[1] if out is not None else None, "out[1]", here, (*x.shape[:-1], d // 32), torch.uint8, x.device)
     _check(load_library().maxscore_mxfp4_quantise(ptr, code, x.numel() // d, d, _ptr(q), _ptr(scales), _stream()), "maxscore_mxfp4_quantise")
     return q, scales
 
 
 def mxfp4_dequantise(q, scales, dtype=None, out=None):
     """The values [..., d] (bf16, or `dtype` fp32) of rows in four bits."""
-    torch = _torch()
+    here = _here()
+    torch = _TORCH
     if q.dim() < 1 or q.numel() == 0 or q.shape[-1] % 16:
         raise MaxScoreError(ERR_SHAPE, "q: rows of a multiple of 16 bytes expected")
     d = 2 * q.shape[-1]
-    ptrs = (_operand(q, "q", None, torch.uint8), _operand(scales, "scales", (*q.shape[:-1], d // 32), torch.uint8))
-    x = _result(out, "out", (*q.shape[:-1], d), dtype if dtype is not None else out.dtype if out is not None else torch.bfloat16, q.device)
+    ptrs = (_operand(q, "q", here, None, torch.uint8), _operand(scales, "scales", here, (*q.shape[:-1], d // 32), torch.uint8))
+    x = _result(out, "out", here, (*q.shape[:-1], d), dtype if dtype is not None else out.dtype if out is not None else torch.bfloat16, q.device)
     _check(load_library().maxscore_mxfp4_dequantise(*ptrs, q.numel() * 2 // d, d, _dtype_code(x), _ptr(x), _stream()), "maxscore_mxfp4_dequantise")
     return x
 
 
 def _mxfp4_product(entry, gated, xq, xs, wq, ws, expert_offsets, out):
-    torch = _torch()
+    here = _here()
+    torch = _TORCH
     E, C, half = _buffer(xq, "xq")
     rows = _buffer(wq, "wq")[1]
     if half % 16 or (gated and rows % 2):
         raise MaxScoreError(ERR_SHAPE, "xq, wq: rows of a multiple of 16 bytes, and as many gate as up rows, expected")
-    ptrs = (_operand(xq, "xq", None, torch.uint8), _operand(xs, "xs", (E, C, half // 16), torch.uint8),
-            _operand(wq, "wq", (E, rows, half), torch.uint8), _operand(ws, "ws", (E, rows, half // 16), torch.uint8), _offsets_of(expert_offsets, E))
+    ptrs = (_operand(xq, "xq", here, None, torch.uint8), _operand(xs, "xs", here, (E, C, half // 16), torch.uint8),
+            _operand(wq, "wq", here, (E, rows, half), torch.uint8), _operand(ws, "ws", here, (E, rows, half // 16), torch.uint8), _offsets_of(expert_offsets, here, E))
     N = rows // 2 if gated else rows
-    y = _result(out, "out", (E, C, N), torch.bfloat16, xq.device)
+    y = _result(out, "out", here, (E, C, N), torch.bfloat16, xq.device)
     _check(getattr(load_library(), entry)(*ptrs, E, C, 2 * half, N, _ptr(y), _stream()), entry)
     return y
 

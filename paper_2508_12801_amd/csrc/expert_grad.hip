@@ -24,28 +24,31 @@ __device__ __forceinline__ int filled_rows(const int32_t *__restrict__ offsets, 
 }
 
 // h = u g s, dg = dh u s (1 + g (1 - s)), du = dh g s with s = 1 / (1 + e^-g), all from gate_up's and dh's rounded values in fp32.
-template <typename T>
+// A thread takes PER neighbouring columns of a row (16 bytes, or one of them where rows are no whole numbers of these); bound by HBM.
+template <typename T, int PER>
 __global__ __launch_bounds__(256) void k_swiglu_backward(const T *__restrict__ gate_up, const T *__restrict__ dh, const int32_t *__restrict__ offsets,
-                                                         int E, int C, int N, T *__restrict__ dgate_up, T *__restrict__ h)
+                                                         unsigned row0, unsigned rows, int C, int N, T *__restrict__ dgate_up, T *__restrict__ h)
 {
-    const size_t rows = (size_t)E * C;
-    for (size_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        const int j = (int)(r / C), m = (int)(r - (size_t)j * C);
-        const bool has = m < filled_rows(offsets, j, C);
-        for (int n = threadIdx.x; n < N; n += 256) {
-            float dg = 0.f, du = 0.f, hv = 0.f;
-            if (has) {
-                const float g = to_f32(gate_up[r * 2 * N + n]), u = to_f32(gate_up[r * 2 * N + N + n]), d = to_f32(dh[r * N + n]);
-                const float s = 1.f / (1.f + expf(-g)), gs = g * s;
-                hv = u * gs;
-                du = d * gs;
-                dg = d * u * s * fmaf(g, 1.f - s, 1.f);
-            }
-            dgate_up[r * 2 * N + n] = from_f32<T>(dg);
-            dgate_up[r * 2 * N + N + n] = from_f32<T>(du);
-            if (h) h[r * N + n] = from_f32<T>(hv);
+    struct __attribute__((aligned(PER * sizeof(T)))) Piece { T v[PER]; };
+    const unsigned pieces = (unsigned)N / PER, at = blockIdx.x * 256u + threadIdx.x, r = at / pieces;
+    if (r >= rows) return;
+    const unsigned row = row0 + r, n = (at - r * pieces) * PER, j = row / (unsigned)C;
+    const bool has = (int)(row - j * C) < filled_rows(offsets, j, C);
+    const size_t gate_at = (size_t)row * 2 * N + n, dh_at = (size_t)row * N + n;
+    Piece dg = {}, du = {}, hv = {};
+    if (has) {
+        const Piece g = *(const Piece *)(gate_up + gate_at), u = *(const Piece *)(gate_up + gate_at + N), d = *(const Piece *)(dh + dh_at);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const float gv = to_f32(g.v[i]), uv = to_f32(u.v[i]), dv = to_f32(d.v[i]), s = 1.f / (1.f + expf(-gv)), gs = gv * s;
+            hv.v[i] = from_f32<T>(uv * gs);
+            du.v[i] = from_f32<T>(dv * gs);
+            dg.v[i] = from_f32<T>(dv * uv * s * fmaf(gv, 1.f - s, 1.f));
         }
     }
+    *(Piece *)(dgate_up + gate_at) = dg;
+    *(Piece *)(dgate_up + gate_at + N) = du;
+    if (h) *(Piece *)(h + dh_at) = hv;
 }
 
 // The sum over the wavefront's lanes, as a tree: within sixteen lanes by lane moves, the four rows' sums one by one.
@@ -204,13 +207,22 @@ __global__ __launch_bounds__(256) void k_combine_backward_elem(const float *__re
 int32_t swiglu_backward_run(const void *gate_up, const void *dh, int dtype, const int32_t *offsets, int E, int C, int N, void *dgate_up, void *h,
                             hipStream_t s)
 {
-    const unsigned grid = (unsigned)std::min<size_t>((size_t)E * C, 1 << 22);
-    if (dtype == MAXSCORE_DTYPE_BF16)
-        hipLaunchKernelGGL((k_swiglu_backward<unsigned short>), dim3(grid), dim3(256), 0, s, (const unsigned short *)gate_up, (const unsigned short *)dh,
-                           offsets, E, C, N, (unsigned short *)dgate_up, (unsigned short *)h);
-    else
-        hipLaunchKernelGGL((k_swiglu_backward<float>), dim3(grid), dim3(256), 0, s, (const float *)gate_up, (const float *)dh, offsets, E, C, N,
-                           (float *)dgate_up, (float *)h);
+    const int size = dtype == MAXSCORE_DTYPE_BF16 ? 2 : 4;
+    const bool vec = (size_t)N * size % 16 == 0 && (((uintptr_t)gate_up | (uintptr_t)dh | (uintptr_t)dgate_up | (uintptr_t)h) % 16) == 0;
+    const unsigned rows = (unsigned)E * (unsigned)C, pieces = vec ? N * size / 16 : N;      // E <= 2^10, C <= 2^21
+    const unsigned most = (1u << 31) / pieces;                                             // rows a launch (its threads are counted in 32 bits)
+    for (unsigned r0 = 0; r0 < rows; r0 += most) {
+        const unsigned n = std::min(most, rows - r0);
+#define MS_SWIGLU_B(TT, PP)                                                                                                                     \
+    hipLaunchKernelGGL((k_swiglu_backward<TT, PP>), dim3((unsigned)(((size_t)n * pieces + 255) / 256)), dim3(256), 0, s, (const TT *)gate_up,       \
+                       (const TT *)dh, offsets, r0, n, C, N, (TT *)dgate_up, (TT *)h)
+        if (size == 2 && vec) MS_SWIGLU_B(unsigned short, 8);
+        else if (size == 2) MS_SWIGLU_B(unsigned short, 1);
+        else if (vec) MS_SWIGLU_B(float, 4);
+        else MS_SWIGLU_B(float, 1);
+#undef MS_SWIGLU_B
+        if (rows - r0 <= most) break;                       // (r0 + most may pass 32 bits)
+    }
     MS_HIP(hipGetLastError());
     return MAXSCORE_OK;
 }

@@ -87,6 +87,7 @@ class Tensor:
 @pytest.fixture
 def bound(monkeypatch):
     monkeypatch.setattr(binding, "_torch", lambda: FakeCuda())
+    monkeypatch.setattr(binding, "_TORCH", torch)
     monkeypatch.setattr(binding, "_stream", lambda: None)
     launched = []
 
