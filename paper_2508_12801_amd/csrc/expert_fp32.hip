@@ -4,23 +4,12 @@
 #include "expert_tile.h"
 
 namespace maxscore {
-namespace {
-
-template <bool COLS_B, bool WGRAD, int END>
-int32_t run(const ExpertArgs &p, hipStream_t s)
-{
-    if (ex_aligned<kExpFp32>(p, COLS_B, WGRAD, END == kExpSwiglu || END == kExpSwigluKeep)) return ex_launch<kExpFp32, COLS_B, WGRAD, END, true, 2, 2, 2, 2, 2>(p, s);
-    return ex_launch<kExpFp32, COLS_B, WGRAD, END, false, 2, 2, 2, 2, 2>(p, s);
-}
-
-}  // namespace
-
 int32_t expert_product_fp32(bool cols_b, bool wgrad, ExpertEnd end, ExpertArgs p, hipStream_t s)
 {
-    if (wgrad) return end == kExpStoreFp32 ? run<true, true, kExpStoreFp32>(p, s) : run<true, true, kExpStore>(p, s);
-    if (end == kExpStore) return cols_b ? run<true, false, kExpStore>(p, s) : run<false, false, kExpStore>(p, s);
-    if (end == kExpSwiglu) return cols_b ? run<true, false, kExpSwiglu>(p, s) : run<false, false, kExpSwiglu>(p, s);
-    return cols_b ? run<true, false, kExpSwigluKeep>(p, s) : run<false, false, kExpSwigluKeep>(p, s);
+    if (wgrad) return end == kExpStoreFp32 ? ex_run<kExpFp32, true, true, kExpStoreFp32>(p, s) : ex_run<kExpFp32, true, true, kExpStore>(p, s);
+    if (end == kExpStore) return cols_b ? ex_run<kExpFp32, true, false, kExpStore>(p, s) : ex_run<kExpFp32, false, false, kExpStore>(p, s);
+    if (end == kExpSwiglu) return cols_b ? ex_run<kExpFp32, true, false, kExpSwiglu>(p, s) : ex_run<kExpFp32, false, false, kExpSwiglu>(p, s);
+    return cols_b ? ex_run<kExpFp32, true, false, kExpSwigluKeep>(p, s) : ex_run<kExpFp32, false, false, kExpSwigluKeep>(p, s);
 }
 
 }  // namespace maxscore

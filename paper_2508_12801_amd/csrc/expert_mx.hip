@@ -4,20 +4,9 @@
 #include "expert_tile.h"
 
 namespace maxscore {
-namespace {
-
-template <int END>
-int32_t run(const ExpertArgs &p, hipStream_t s)
-{
-    if (ex_aligned<kExpMx>(p, false, false, END == kExpSwiglu)) return ex_launch<kExpMx, false, false, END, true, 2, 2, 2, 2, 2>(p, s);
-    return ex_launch<kExpMx, false, false, END, false, 2, 2, 2, 2, 2>(p, s);
-}
-
-}  // namespace
-
 int32_t expert_product_mx(ExpertEnd end, ExpertArgs p, hipStream_t s)
 {
-    return end == kExpSwiglu ? run<kExpSwiglu>(p, s) : run<kExpStore>(p, s);
+    return end == kExpSwiglu ? ex_run<kExpMx, false, false, kExpSwiglu>(p, s) : ex_run<kExpMx, false, false, kExpStore>(p, s);
 }
 
 }  // namespace maxscore

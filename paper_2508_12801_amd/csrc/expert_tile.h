@@ -73,7 +73,9 @@ __device__ __forceinline__ void ex_load_lds(const char *base, unsigned off, unsi
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
 }
-__device__ __forceinline__ void ex_loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// Waits until no more than LEFT of the wavefront's loads are on their way: they end in the order in which they began.
+template <int LEFT>
+__device__ __forceinline__ void ex_loads_done() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory"); }
 
 // How far the chunks of row k of a slab of cols are turned.
 template <int F, int R>
@@ -203,19 +205,20 @@ __device__ __forceinline__ void ex_put_rows(char *scratch, void *out, int m, int
 // WM x WN wavefronts, each with TM x TN blocks of 32 x 32.  The gated unit takes gate and up columns by turns of 32, so that a wavefront
 // has both of an h in the same lane and register.
 //
-// Two slabs in LDS: the next one is on its way, past the registers, while the matrix instructions work on this one, and one barrier a slab keeps them
-// apart.  A slab that ends early, and every slab of rows that are no whole numbers of 16 bytes, is filled in through registers, zero where there is nothing;
+// STAGES slabs in LDS: the next ones are on their way, past the registers, while the matrix instructions work on this one, and one barrier a slab keeps
+// them apart (a buffer is filled again once all wavefronts are past the barrier behind its use).  A slab that ends early, and every slab of rows that are no whole numbers of 16 bytes, is filled in through registers, zero where there is nothing;
 // rows and columns of the tile that the result does not have are copies of its last ones.
-template <int F, bool COLS_B, bool WGRAD, int END, bool ALIGNED, int WM, int WN, int TM, int TN, int WGS>
+template <int F, bool COLS_B, bool WGRAD, int END, bool ALIGNED, int WM, int WN, int TM, int TN, int STAGES, int WGS>
 __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_product(ExpertArgs p)
 {
     constexpr int NT = 64 * WM * WN, BM = 32 * WM * TM, BN = 32 * WN * TN, CE = ExpertElem<F>::chunk, KS = kSlabBytes / 16 * CE;
     constexpr bool GATED = END == kExpSwiglu || END == kExpSwigluKeep, OUT32 = F == kExpFp32 || END == kExpStoreFp32, MX = F == kExpMx;
     constexpr bool COLS_A = WGRAD;
     constexpr int SLAB = (BM + BN) * kSlabBytes, SCALES = MX ? (BM + BN) * 8 : 0;
+    static_assert(!MX || STAGES == 2, "a slab's scales wait in registers for all loads before them");
     static_assert(!GATED || TN % 2 == 0, "gate and up in one wavefront");
     static_assert(BM * 8 % NT == 0 && BN * 8 % NT == 0, "as many loads to every wavefront");
-    __shared__ __attribute__((aligned(1024))) char s_mem[2 * (SLAB + SCALES)];
+    __shared__ __attribute__((aligned(1024))) char s_mem[STAGES * (SLAB + SCALES)];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
 
     // Workgroups go to the eight dies in turn; a die takes `together` neighbouring tiles, whose operands meet in its L2.
@@ -291,7 +294,7 @@ __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_prod
         auto put_scales = [&](int buf) {
 #pragma unroll
             for (int i = 0; i < NSC; ++i)
-                if (tid + i * NT < BM + BN) *(unsigned long long *)(s_mem + 2 * SLAB + buf * SCALES + (tid + i * NT) * 8) = sc[i];
+                if (tid + i * NT < BM + BN) *(unsigned long long *)(s_mem + STAGES * SLAB + buf * SCALES + (tid + i * NT) * 8) = sc[i];
         };
         auto fill = [&](int slab, int buf) {
             char *s_a = s_mem + buf * SLAB, *s_b = s_a + BM * kSlabBytes;
@@ -320,7 +323,7 @@ __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_prod
         };
         const bool busy = m0 + wm * TM * 32 < ms;           // the others have nothing but rows that the result does not have
         auto compute = [&](int buf) {
-            const char *s_a = s_mem + buf * SLAB, *s_b = s_a + BM * kSlabBytes, *s_sa = s_mem + 2 * SLAB + buf * SCALES, *s_sb = s_sa + BM * 8;
+            const char *s_a = s_mem + buf * SLAB, *s_b = s_a + BM * kSlabBytes, *s_sa = s_mem + STAGES * SLAB + buf * SCALES, *s_sb = s_sa + BM * 8;
             int va[TM], vb[TN];
 #pragma unroll
             for (int i = 0; i < TM; ++i) va[i] = MX ? *(const int *)(s_sa + (wm * TM * 32 + i * 32 + (lane & 31)) * 8 + 4 * (lane >> 5)) : 0;
@@ -344,17 +347,21 @@ __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_prod
             step(std::integral_constant<int, 3>{});
         };
         const int slabs = (ks + KS - 1) / KS, whole = ALIGNED ? ks / KS : 0;
-        if (whole > 0) fetch(0, 0);
-        for (int i = 0; i < slabs; ++i) {
+#pragma unroll
+        for (int i = 0; i < STAGES - 1; ++i)
+            if (i < whole) fetch(i, i);
+        for (int i = 0, buf = 0; i < slabs; ++i) {
             if (i < whole) {
-                ex_loads_done();
-                if constexpr (MX) put_scales(i & 1);
+                if (i + STAGES - 1 <= whole) ex_loads_done<(STAGES - 2) * (NA + NB)>();
+                else ex_loads_done<0>();
+                if constexpr (MX) put_scales(buf);
             } else {
-                fill(i, i & 1);
+                fill(i, buf);
             }
             __syncthreads();
-            if (i + 1 < whole) fetch(i + 1, (i + 1) & 1);
-            if (busy) compute(i & 1);
+            if (i + STAGES - 1 < whole) fetch(i + STAGES - 1, buf == 0 ? STAGES - 1 : buf - 1);
+            if (busy) compute(buf);
+            buf = buf == STAGES - 1 ? 0 : buf + 1;
         }
     }
 
@@ -393,7 +400,12 @@ __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_prod
     }
 }
 
-template <int F, bool COLS_B, bool WGRAD, int END, bool ALIGNED, int WM, int WN, int TM, int TN, int WGS>
+// The tiles, by what a call has of them.  256 x 256 has the most operations to a byte (64 x 2048 rows of bf16, 2048 to 1024: 524 us, 611 with 128 x 128; of
+// four bits 197 and 252) but is alone on its compute unit: only where it fills all of them (16 x 512 rows, 1024 to 1024: 128 tiles take 32 us, 512 of 128 x 128
+// 23).  64 x 128, FIXME
+long long ex_tiles(const ExpertArgs &p, int bm, int bn) { return (long long)((p.M + bm - 1) / bm) * ((p.N + bn - 1) / bn) * p.E; }
+
+template <int F, bool COLS_B, bool WGRAD, int END, bool ALIGNED, int WM, int WN, int TM, int TN, int STAGES, int WGS>
 int32_t ex_launch(ExpertArgs p, hipStream_t s)
 {
     constexpr bool GATED = END == kExpSwiglu || END == kExpSwigluKeep;
@@ -404,7 +416,7 @@ int32_t ex_launch(ExpertArgs p, hipStream_t s)
     p.together = (int)std::min<long long>(kTilesTogether, (real + 7) / 8);          // few tiles: an equal share to every die
     const long long all = 8 * p.together, tiles = (real + all - 1) / all * all;
     if (tiles > 0xffffffffll / (64 * WM * WN)) return MAXSCORE_ERR_SHAPE;      // a launch counts its threads in 32 bits
-    hipLaunchKernelGGL((k_expert_product<F, COLS_B, WGRAD, END, ALIGNED, WM, WN, TM, TN, WGS>), dim3((unsigned)tiles), dim3(64 * WM * WN), 0, s, p);
+    hipLaunchKernelGGL((k_expert_product<F, COLS_B, WGRAD, END, ALIGNED, WM, WN, TM, TN, STAGES, WGS>), dim3((unsigned)tiles), dim3(64 * WM * WN), 0, s, p);
     MS_HIP(hipGetLastError());
     return MAXSCORE_OK;
 }
@@ -419,6 +431,21 @@ bool ex_aligned(const ExpertArgs &p, bool cols_b, bool wgrad, bool gated)
     if (at % 16 || p.N % (F == kExpMx ? 8 : CE)) return false;
     if (gated && !cols_b && ((long long)p.N + 256) * p.K * 16 / CE >> 32) return false;
     return wgrad ? p.M % CE == 0 : p.K % CE == 0;
+}
+
+template <int F, bool COLS_B, bool WGRAD, int END>
+int32_t ex_run(const ExpertArgs &p, hipStream_t s)
+{
+    constexpr bool GATED = END == kExpSwiglu || END == kExpSwigluKeep;
+    if (!ex_aligned<F>(p, COLS_B, WGRAD, GATED)) return ex_launch<F, COLS_B, WGRAD, END, false, 2, 2, 2, 2, 2, 2>(p, s);
+    if (!WGRAD && p.M <= 64) {
+        if constexpr (F == kExpMx) return ex_launch<F, COLS_B, WGRAD, END, true, 2, 2, 1, 2, 2, 3>(p, s);
+        else if (ex_tiles(p, 64, GATED ? 64 : 128) > 256) return ex_launch<F, COLS_B, WGRAD, END, true, 2, 2, 1, 2, 3, 2>(p, s);
+        else return ex_launch<F, COLS_B, WGRAD, END, true, 2, 2, 1, 2, 6, 1>(p, s);
+    }
+    if constexpr (F != kExpFp32)
+        if (ex_tiles(p, 256, GATED ? 128 : 256) >= 256) return ex_launch<F, COLS_B, WGRAD, END, true, 2, 4, 4, 2, 2, 1>(p, s);
+    return ex_launch<F, COLS_B, WGRAD, END, true, 2, 2, 2, 2, 2, 2>(p, s);
 }
 
 }  // namespace
