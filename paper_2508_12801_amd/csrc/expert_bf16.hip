@@ -1,9 +1,10 @@
 // The experts' products in bf16: 32x32x16, eight passes for 32768 operations; sums in fp32, rounded once.
 #include <type_traits>
 
-#include "expert_tile.h"
+#include "expert_run.h"
 
 namespace maxscore {
+
 int32_t expert_product_bf16(bool cols_b, bool wgrad, ExpertEnd end, ExpertArgs p, hipStream_t s)
 {
     if (wgrad) return end == kExpStoreFp32 ? ex_run<kExpBf16, true, true, kExpStoreFp32>(p, s) : ex_run<kExpBf16, true, true, kExpStore>(p, s);

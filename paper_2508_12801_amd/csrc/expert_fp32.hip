@@ -1,9 +1,10 @@
 // The experts' products in fp32 throughout, on the matrix cores (32x32x2).
 #include <type_traits>
 
-#include "expert_tile.h"
+#include "expert_run.h"
 
 namespace maxscore {
+
 int32_t expert_product_fp32(bool cols_b, bool wgrad, ExpertEnd end, ExpertArgs p, hipStream_t s)
 {
     if (wgrad) return end == kExpStoreFp32 ? ex_run<kExpFp32, true, true, kExpStoreFp32>(p, s) : ex_run<kExpFp32, true, true, kExpStore>(p, s);

@@ -250,7 +250,7 @@ __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_prod
         const unsigned char *sa = MX ? p.sa + (size_t)j * p.C * blocks : nullptr, *sb = MX ? p.sb + (size_t)j * n_all * blocks : nullptr;
         const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)s_mem + wave * 1024;
         constexpr int NA = BM * 8 / NT, NB = BN * 8 / NT, NSC = MX ? (BM + BN + NT - 1) / NT : 1;
-        unsigned off_a[NA], off_b[NB];
+        unsigned off_a[NA] = {}, off_b[NB] = {};
         const char *tile_a = a + (COLS_A ? (size_t)m0 * 16 / CE : m0 * row_a), *tile_b = b + (COLS_B ? (size_t)n0 * 16 / CE : n0 * row_b);
         const size_t next_a = COLS_A ? KS * row_a : kSlabBytes, next_b = COLS_B ? KS * row_b : kSlabBytes;
         if constexpr (ALIGNED) {
@@ -270,6 +270,11 @@ __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_prod
                 off_b[i] = COLS_B ? (unsigned)(row * row_b) + d * 16 / CE : (unsigned)(d * row_b) + col * 16 / CE;
             }
         }
+        // (as they are, 32 bits each: not as halves of the products that they come from)
+#pragma unroll
+        for (int i = 0; i < NA; ++i) asm volatile("" : "+v"(off_a[i]));
+#pragma unroll
+        for (int i = 0; i < NB; ++i) asm volatile("" : "+v"(off_b[i]));
         // the scales of a slab, eight bytes to a row of the tile, on their way in registers
         unsigned long long sc[NSC];
         const unsigned char *row_s[NSC];
@@ -400,22 +405,25 @@ __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_prod
     }
 }
 
-// The tiles, by what a call has of them.  256 x 256 has the most operations to a byte (64 x 2048 rows of bf16, 2048 to 1024: 524 us, 611 with 128 x 128; of
-// four bits 197 and 252) but is alone on its compute unit: only where it fills all of them (16 x 512 rows, 1024 to 1024: 128 tiles take 32 us, 512 of 128 x 128
-// 23).  64 x 128, FIXME
-long long ex_tiles(const ExpertArgs &p, int bm, int bn) { return (long long)((p.M + bm - 1) / bm) * ((p.N + bn - 1) / bn) * p.E; }
+// The tiles of a call and their shares for the dies; whether a launch counts so many threads (32 bits).
+bool ex_divide(ExpertArgs &p, int bm, int bn, int threads, long long &tiles)
+{
+    p.mt = (p.M + bm - 1) / bm;
+    p.nt = (p.N + bn - 1) / bn;
+    const long long real = (long long)p.mt * p.nt * p.E;
+    p.together = (int)std::min<long long>(kTilesTogether, (real + 7) / 8);          // few tiles: an equal share to every die
+    const long long all = 8 * p.together;
+    tiles = (real + all - 1) / all * all;
+    return tiles <= 0xffffffffll / threads;
+}
 
 template <int F, bool COLS_B, bool WGRAD, int END, bool ALIGNED, int WM, int WN, int TM, int TN, int STAGES, int WGS>
 int32_t ex_launch(ExpertArgs p, hipStream_t s)
 {
     constexpr bool GATED = END == kExpSwiglu || END == kExpSwigluKeep;
     constexpr int BM = 32 * WM * TM, BN = 32 * WN * TN / (GATED ? 2 : 1);
-    p.mt = (p.M + BM - 1) / BM;
-    p.nt = (p.N + BN - 1) / BN;
-    const long long real = (long long)p.mt * p.nt * p.E;
-    p.together = (int)std::min<long long>(kTilesTogether, (real + 7) / 8);          // few tiles: an equal share to every die
-    const long long all = 8 * p.together, tiles = (real + all - 1) / all * all;
-    if (tiles > 0xffffffffll / (64 * WM * WN)) return MAXSCORE_ERR_SHAPE;      // a launch counts its threads in 32 bits
+    long long tiles;
+    if (!ex_divide(p, BM, BN, 64 * WM * WN, tiles)) return MAXSCORE_ERR_SHAPE;
     hipLaunchKernelGGL((k_expert_product<F, COLS_B, WGRAD, END, ALIGNED, WM, WN, TM, TN, STAGES, WGS>), dim3((unsigned)tiles), dim3(64 * WM * WN), 0, s, p);
     MS_HIP(hipGetLastError());
     return MAXSCORE_OK;
@@ -431,21 +439,6 @@ bool ex_aligned(const ExpertArgs &p, bool cols_b, bool wgrad, bool gated)
     if (at % 16 || p.N % (F == kExpMx ? 8 : CE)) return false;
     if (gated && !cols_b && ((long long)p.N + 256) * p.K * 16 / CE >> 32) return false;
     return wgrad ? p.M % CE == 0 : p.K % CE == 0;
-}
-
-template <int F, bool COLS_B, bool WGRAD, int END>
-int32_t ex_run(const ExpertArgs &p, hipStream_t s)
-{
-    constexpr bool GATED = END == kExpSwiglu || END == kExpSwigluKeep;
-    if (!ex_aligned<F>(p, COLS_B, WGRAD, GATED)) return ex_launch<F, COLS_B, WGRAD, END, false, 2, 2, 2, 2, 2, 2>(p, s);
-    if (!WGRAD && p.M <= 64) {
-        if constexpr (F == kExpMx) return ex_launch<F, COLS_B, WGRAD, END, true, 2, 2, 1, 2, 2, 3>(p, s);
-        else if (ex_tiles(p, 64, GATED ? 64 : 128) > 256) return ex_launch<F, COLS_B, WGRAD, END, true, 2, 2, 1, 2, 3, 2>(p, s);
-        else return ex_launch<F, COLS_B, WGRAD, END, true, 2, 2, 1, 2, 6, 1>(p, s);
-    }
-    if constexpr (F != kExpFp32)
-        if (ex_tiles(p, 256, GATED ? 128 : 256) >= 256) return ex_launch<F, COLS_B, WGRAD, END, true, 2, 4, 4, 2, 2, 1>(p, s);
-    return ex_launch<F, COLS_B, WGRAD, END, true, 2, 2, 2, 2, 2, 2>(p, s);
 }
 
 }  // namespace
