@@ -16,23 +16,30 @@
 namespace maxscore {
 namespace {
 
-template <int VM>
+// Until at most VM of the wavefront's loads are on their way, and all wavefronts are here.  FENCE: matrix instructions stay on their side.  Those of four
+// bits, moved, keep two quarters' operands in registers (300 of them spilled); for bf16 moving is better (64 x 4096 rows, 2048 to 2048: 1852 us, 1896 so).
+template <int VM, bool FENCE>
 __device__ __forceinline__ void ex_meet()
 {
+    if (FENCE) __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(VM) : "memory");
+    if (FENCE) __builtin_amdgcn_sched_barrier(0);
 }
 
 enum { kPartA0, kPartA1, kPartB0, kPartB1 };
 // Where a part of an even or odd slab lies: all of A's within what an instruction's own offset reaches, and all of B's.
 __device__ constexpr int ex_slot(int part, int parity) { return (part / 2 * 4 + parity * 2 + part % 2) * 128 * kSlabBytes; }
 
-template <int F, bool COLS_B, bool WGRAD, int END>
+// Four bits: the scales of two slabs come together, 16 bytes to a row of the tile (A's 256, then B's), a load a thread; LDS has those of two and two.
+constexpr int kScalesTwo = 512 * 16;
+
+template <int F, bool COLS_B, bool WGRAD, int END, bool PAST>
 __global__ __launch_bounds__(512, 2) void k_expert_big(ExpertArgs p)
 {
     constexpr int CE = ExpertElem<F>::chunk, KS = kSlabBytes / 16 * CE, PART = 128 * kSlabBytes;
-    constexpr bool GATED = END == kExpSwiglu || END == kExpSwigluKeep, OUT32 = F == kExpFp32 || END == kExpStoreFp32, COLS_A = WGRAD;
-    static_assert(F != kExpMx, "scales");
-    __shared__ __attribute__((aligned(1024))) char s_mem[8 * PART];
+    constexpr bool GATED = END == kExpSwiglu || END == kExpSwigluKeep, OUT32 = F == kExpFp32 || END == kExpStoreFp32, COLS_A = WGRAD,
+                   MX = F == kExpMx;
+    __shared__ __attribute__((aligned(1024))) char s_mem[8 * PART + (MX ? 2 * kScalesTwo : 0)];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 2, wn = wave & 3;
 
     const unsigned die = blockIdx.x & 7u, turn = blockIdx.x >> 3;
@@ -88,6 +95,32 @@ __global__ __launch_bounds__(512, 2) void k_expert_big(ExpertArgs p)
 #pragma unroll
             for (int i = 0; i < 2; ++i) ex_load_lds(base, off[part][i], lds + ex_slot(part, parity) + i * 8192);
         };
+        const int blocks = p.K / 32;
+        unsigned off_s = 0;
+        const char *tile_s = nullptr;
+        if constexpr (MX) {
+            const int r = tid & 255;
+            if (wave < 4) {
+                tile_s = (const char *)p.sa + ((size_t)j * p.C + m0) * blocks;
+                off_s = (unsigned)((m0 + r < ms ? r : ms - 1 - m0) * blocks);
+            } else {
+                tile_s = (const char *)p.sb + ((size_t)j * n_all + n0) * blocks;
+                const int rb = b_index(r >> 7, r & 127);
+                off_s = (unsigned)((rb < n_all ? rb : n_all - 1) - n0) * (unsigned)blocks;
+            }
+        }
+        auto ask_scales = [&](int slab) { ex_load_lds(tile_s + slab * 8, off_s, lds + 8 * PART + (slab >> 1 & 1) * kScalesTwo); };
+        int va[2][2] = {}, vb[2] = {};                // the lane's scales, a byte a step
+        auto read_scales = [&](auto part_, int slab) {
+            constexpr int part = decltype(part_)::value;
+            const char *at = s_mem + 8 * PART + (slab >> 1 & 1) * kScalesTwo + (slab & 1) * 8 + (lane & 31) * 16 + (lane >> 5) * 4;
+            if constexpr (part < kPartB0) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) va[part][i] = *(const int *)(at + ((part & 1) * 128 + (wm * 2 + i) * 32) * 16);
+            } else {
+                vb[part & 1] = *(const int *)(at + (256 + (part & 1) * 128 + wn * 32) * 16);
+            }
+        };
         ExpertFrag<F> fa[2][2][4], fb[2][4];          // [part][block][step]
         unsigned place[4];                            // of rows: a lane's chunk of its row in step kk
         // of cols: k's row and the chunk in it but for the block, and what turns that
@@ -95,7 +128,8 @@ __global__ __launch_bounds__(512, 2) void k_expert_big(ExpertArgs p)
         place_cols |= ((lane & 15) >> 2) << 16;
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) place[kk] = (lane & 31) * kSlabBytes + (((4 * (lane >> 5) + kk) ^ (lane >> 1 & 7)) << 4);
-        auto read = [&](auto part_, int parity) {
+        auto read = [&](auto part_, int parity, int slab) {
+            if constexpr (MX) read_scales(part_, slab);
             constexpr int part = decltype(part_)::value;
             constexpr bool COLS = part < kPartB0 ? COLS_A : COLS_B;
             constexpr int BLOCKS = part < kPartB0 ? 2 : 1;
@@ -114,7 +148,7 @@ __global__ __launch_bounds__(512, 2) void k_expert_big(ExpertArgs p)
                         const ex_bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_quad)(slot + at + kk * 2048)),
                                         hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_quad)(slot + at + kk * 2048 + 1024));
                         ExpertFrag<F> &f = part < kPartB0 ? fa[part & 1][i][kk] : fb[part & 1][kk];
-                        f.v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                        f.v = __builtin_bit_cast(decltype(f.v), __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
                     }
                 }
             } else {
@@ -133,10 +167,15 @@ __global__ __launch_bounds__(512, 2) void k_expert_big(ExpertArgs p)
         };
         auto quarter = [&](auto ha_, auto hb_) {
             constexpr int ha = decltype(ha_)::value, hb = decltype(hb_)::value;
+            auto step = [&](auto kk) {                // the blocks by turns: a sum is not ready for its next step at once
+                constexpr int KK = decltype(kk)::value;
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) acc[ha][i][hb] = ex_mma<F, 0>(fb[hb][kk], fa[ha][i][kk], acc[ha][i][hb], 0, 0);
+                for (int i = 0; i < 2; ++i) acc[ha][i][hb] = ex_mma<F, KK>(fb[hb][KK], fa[ha][i][KK], acc[ha][i][hb], vb[hb], va[ha][i]);
+            };
+            step(std::integral_constant<int, 0>{});
+            step(std::integral_constant<int, 1>{});
+            step(std::integral_constant<int, 2>{});
+            step(std::integral_constant<int, 3>{});
         };
         constexpr std::integral_constant<int, 0> zero;
         constexpr std::integral_constant<int, 1> one;
@@ -149,46 +188,49 @@ __global__ __launch_bounds__(512, 2) void k_expert_big(ExpertArgs p)
 
         const int slabs = (ks + KS - 1) / KS, whole = ks / KS, even = whole & ~1;
         if (even) {
+            if constexpr (MX) ask_scales(0);
             ask(kPartA0, 0, 0), ask(kPartB0, 0, 0), ask(kPartB1, 0, 0), ask(kPartA1, 0, 0);
             ask(kPartA0, 1, 1), ask(kPartB1, 1, 1), ask(kPartB0, 1, 1), ask(kPartA1, 1, 1);
-            ex_meet<12>();
-            read(A0, 0), read(B0, 0);
+            ex_meet<12, MX>();
+            read(A0, 0, 0), read(B0, 0, 0);
             if (even > 2) {
-                ex_meet<12>();
+                ex_meet<12, MX>();
                 ask(kPartA0, 2, 0);
             }
             auto two_slabs = [&](int e, auto more) {
-                ex_meet<12>();
-                ask(kPartB0, e + 2, 0), read(B1, 0);
+                ex_meet<12, MX>();
+                ask(kPartB0, e + 2, 0);
+                if constexpr (MX) ask_scales(e + 2);
+                read(B1, 0, e);
                 ahead();
                 quarter(zero, zero);
-                ex_meet<12>();
-                ask(kPartB1, e + 2, 0), read(A1, 0);
+                ex_meet<12, MX>();
+                ask(kPartB1, e + 2, 0), read(A1, 0, e);
                 ahead();
                 quarter(zero, one);
-                ex_meet<12>();
-                ask(kPartA1, e + 2, 0), read(A0, 1);
+                ex_meet<12, MX>();
+                ask(kPartA1, e + 2, 0), read(A0, 1, e + 1);
                 ahead();
                 quarter(one, one);
-                ex_meet<12>();
-                ask(kPartA0, e + 3, 1), read(B1, 1);
+                ex_meet<12, MX>();
+                ask(kPartA0, e + 3, 1), read(B1, 1, e + 1);
                 ahead();
                 quarter(one, zero);
-                ex_meet<12>();
-                ask(kPartB1, e + 3, 1), read(B0, 1);
+                ex_meet<12, MX>();
+                ask(kPartB1, e + 3, 1), read(B0, 1, e + 1);
                 ahead();
                 quarter(zero, one);
-                ex_meet<12>();
-                ask(kPartB0, e + 3, 1), read(A1, 1);
+                ex_meet<12, MX>();
+                ask(kPartB0, e + 3, 1), read(A1, 1, e + 1);
                 ahead();
                 quarter(zero, zero);
-                ex_meet<12>();
-                ask(kPartA1, e + 3, 1), read(A0, 0);
+                ex_meet<MX ? 10 : 12, MX>();                  // the next two slabs' scales, five parts ago
+                ask(kPartA1, e + 3, 1), read(A0, 0, e + 2);
                 ahead();
                 quarter(one, zero);
-                ex_meet<12>();
+                ex_meet<12, MX>();
                 if constexpr (decltype(more)::value) ask(kPartA0, e + 4, 0);
-                read(B0, 0);
+                read(B0, 0, e + 2);
                 ahead();
                 quarter(one, one);
             };
@@ -196,28 +238,28 @@ __global__ __launch_bounds__(512, 2) void k_expert_big(ExpertArgs p)
             for (; e + 4 < even; e += 2) two_slabs(e, std::true_type{});
             if (e + 2 < even) two_slabs(e, std::false_type{});
             // the last two slabs: nothing more to ask for, and fewer loads left each time
-            ex_meet<10>();
-            read(B1, 0);
+            ex_meet<10, MX>();
+            read(B1, 0, even - 2);
             ahead();
             quarter(zero, zero);
-            ex_meet<8>();
-            read(A1, 0);
+            ex_meet<8, MX>();
+            read(A1, 0, even - 2);
             ahead();
             quarter(zero, one);
-            ex_meet<6>();
-            read(A0, 1);
+            ex_meet<6, MX>();
+            read(A0, 1, even - 1);
             ahead();
             quarter(one, one);
-            ex_meet<4>();
-            read(B1, 1);
+            ex_meet<4, MX>();
+            read(B1, 1, even - 1);
             ahead();
             quarter(one, zero);
-            ex_meet<2>();
-            read(B0, 1);
+            ex_meet<2, MX>();
+            read(B0, 1, even - 1);
             ahead();
             quarter(zero, one);
-            ex_meet<0>();
-            read(A1, 1);
+            ex_meet<0, MX>();
+            read(A1, 1, even - 1);
             ahead();
             quarter(zero, zero);
             quarter(one, zero);
@@ -225,7 +267,7 @@ __global__ __launch_bounds__(512, 2) void k_expert_big(ExpertArgs p)
         }
         // an odd slab, and one that ends early
         for (int slab = even; slab < slabs; ++slab) {
-            ex_meet<0>();
+            ex_meet<0, MX>();
             if (slab < whole) {
 #pragma unroll
                 for (int part = 0; part < 4; ++part) ask(part, slab, 0);
@@ -246,8 +288,14 @@ __global__ __launch_bounds__(512, 2) void k_expert_big(ExpertArgs p)
                             COLS_B ? ex_load16<F, true>(b, k0 + row, b_index(h, col), ks, n_all) : ex_load16<F, true>(b, b_index(h, row), k0 + col, n_all, p.K);
                     }
             }
-            ex_meet<0>();
-            read(A0, 0), read(B0, 0), read(B1, 0), read(A1, 0);
+            if constexpr (MX) {
+                unsigned long long v = 0;
+                for (int i = 0; i < 8; ++i)
+                    if (slab * 8 + i < blocks) v |= (unsigned long long)(unsigned char)tile_s[off_s + slab * 8 + i] << (8 * i);
+                *(unsigned long long *)(s_mem + 8 * PART + tid * 16) = v;
+            }
+            ex_meet<0, MX>();
+            read(A0, 0, 0), read(B0, 0, 0), read(B1, 0, 0), read(A1, 0, 0);
             quarter(zero, zero), quarter(zero, one), quarter(one, one), quarter(one, zero);
         }
     }
@@ -268,7 +316,7 @@ __global__ __launch_bounds__(512, 2) void k_expert_big(ExpertArgs p)
                 for (int e = 0; e < 4; ++e) v[e] = has ? acc[h][i][u][4 * q + e] : 0.f;
             };
             if constexpr (GATED) {
-                ex_put_rows<OUT32, true, 32>(scratch, out, m, n, p.M, p.N, lane, [&](int q, float(&v)[4]) {
+                ex_put_rows<OUT32, true, PAST, 32>(scratch, out, m, n, p.M, p.N, lane, [&](int q, float(&v)[4]) {
                     float w[4];
                     sums(0, q, v);
                     sums(1, q, w);
@@ -279,23 +327,23 @@ __global__ __launch_bounds__(512, 2) void k_expert_big(ExpertArgs p)
                     char *keep = (char *)p.keep + (size_t)j * p.M * n_all * SIZE;
 #pragma unroll
                     for (int u = 0; u < 2; ++u)
-                        ex_put_rows<OUT32, true, 32, 2>(scratch, keep + (size_t)u * p.N * SIZE, m, n, p.M, p.N, lane, [&](int q, float(&v)[4]) { sums(u, q, v); });
+                        ex_put_rows<OUT32, true, PAST, 32, 2>(scratch, keep + (size_t)u * p.N * SIZE, m, n, p.M, p.N, lane, [&](int q, float(&v)[4]) { sums(u, q, v); });
                 }
             } else {
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
-                    ex_put_rows<OUT32, true, 32>(scratch, out, m, n + u * 128, p.M, p.N, lane, [&](int q, float(&v)[4]) { sums(u, q, v); });
+                    ex_put_rows<OUT32, true, PAST, 32>(scratch, out, m, n + u * 128, p.M, p.N, lane, [&](int q, float(&v)[4]) { sums(u, q, v); });
             }
         }
 }
 
-template <int F, bool COLS_B, bool WGRAD, int END>
+template <int F, bool COLS_B, bool WGRAD, int END, bool PAST>
 int32_t ex_launch_big(ExpertArgs p, hipStream_t s)
 {
     constexpr int BN = END == kExpSwiglu || END == kExpSwigluKeep ? 128 : 256;
     long long tiles;
     if (!ex_divide(p, 256, BN, 512, tiles)) return MAXSCORE_ERR_SHAPE;
-    hipLaunchKernelGGL((k_expert_big<F, COLS_B, WGRAD, END>), dim3((unsigned)tiles), dim3(512), 0, s, p);
+    hipLaunchKernelGGL((k_expert_big<F, COLS_B, WGRAD, END, PAST>), dim3((unsigned)tiles), dim3(512), 0, s, p);
     MS_HIP(hipGetLastError());
     return MAXSCORE_OK;
 }

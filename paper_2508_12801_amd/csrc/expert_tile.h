@@ -73,6 +73,13 @@ __device__ __forceinline__ void ex_load_lds(const char *base, unsigned off, unsi
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
 }
+// The same from an address of its own for every lane.
+__device__ __forceinline__ void ex_load_lds_from(const char *at, unsigned lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(at) : "memory");
+}
+// What a slab that ends early has behind its end.
+__device__ const ex_u32x4 ex_nothing = {0u, 0u, 0u, 0u};
 // Waits until no more than LEFT of the wavefront's loads are on their way: they end in the order in which they began.
 template <int LEFT>
 __device__ __forceinline__ void ex_loads_done() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory"); }
@@ -161,7 +168,7 @@ __device__ __forceinline__ auto ex_pack4(const float (&v)[4])
 // A wavefront's 32 rows of COLS columns of the result at row m, column n of `out`, rows of PITCH * cols of which `cols` are its.  A lane has four columns of one row at a time
 // (values(q, v): columns 8 q + 4 (lane / 32) .. of row lane % 32), which would be 32 stores to as many lines; through its part of LDS (chunks turned as in a slab) they
 // become whole lines.  Rows that are no whole numbers of 16 bytes are stored value by value.
-template <bool FP32, bool ALIGNED, int COLS, int PITCH = 1, typename V>
+template <bool FP32, bool ALIGNED, bool PAST, int COLS, int PITCH = 1, typename V>
 __device__ __forceinline__ void ex_put_rows(char *scratch, void *out, int m, int n, int rows, int cols, int lane, V values)
 {
     constexpr int SIZE = FP32 ? 4 : 2, CPR = COLS * SIZE / 16, PER = 16 / SIZE, ALL = 32 * CPR;
@@ -181,7 +188,11 @@ __device__ __forceinline__ void ex_put_rows(char *scratch, void *out, int m, int
             const int row = (i + lane) / CPR, c = (i + lane) % CPR;
             if (ALL % 64 && i + lane >= ALL) break;
             const ex_u32x4 x = *(const ex_u32x4 *)(scratch + row * (CPR * 16) + ((c ^ (row >> 1 & (TURN - 1))) << 4));
-            if (m + row < rows && n + c * PER < cols) *(ex_u32x4 *)((char *)out + ((size_t)(m + row) * (PITCH * (size_t)cols) + n + c * PER) * SIZE) = x;
+            ex_u32x4 *to = (ex_u32x4 *)((char *)out + ((size_t)(m + row) * (PITCH * (size_t)cols) + n + c * PER) * SIZE);
+            if (m + row < rows && n + c * PER < cols) {
+                if (PAST) __builtin_nontemporal_store(x, to);
+                else *to = x;
+            }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     } else {
@@ -206,9 +217,9 @@ __device__ __forceinline__ void ex_put_rows(char *scratch, void *out, int m, int
 // has both of an h in the same lane and register.
 //
 // STAGES slabs in LDS: the next ones are on their way, past the registers, while the matrix instructions work on this one, and one barrier a slab keeps
-// them apart (a buffer is filled again once all wavefronts are past the barrier behind its use).  A slab that ends early, and every slab of rows that are no whole numbers of 16 bytes, is filled in through registers, zero where there is nothing;
-// rows and columns of the tile that the result does not have are copies of its last ones.
-template <int F, bool COLS_B, bool WGRAD, int END, bool ALIGNED, int WM, int WN, int TM, int TN, int STAGES, int WGS>
+// them apart (a buffer is filled again once all wavefronts are past the barrier behind its use).  A slab that ends early has zeros behind its end; slabs of rows that are no whole numbers of 16 bytes are filled in through registers.  Rows and
+// columns of the tile that the result does not have are copies of its last ones.
+template <int F, bool COLS_B, bool WGRAD, int END, bool ALIGNED, int WM, int WN, int TM, int TN, int STAGES, int WGS, bool PAST = false>
 __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_product(ExpertArgs p)
 {
     constexpr int NT = 64 * WM * WN, BM = 32 * WM * TM, BN = 32 * WN * TN, CE = ExpertElem<F>::chunk, KS = kSlabBytes / 16 * CE;
@@ -286,7 +297,35 @@ __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_prod
                 else row_s[i] = sb + (size_t)(r < BM + BN && b_index(r - BM) < n_all ? b_index(r - BM) : n_all - 1) * blocks;
             }
         }
+        const int slabs = (ks + KS - 1) / KS, whole = ks / KS;
         auto fetch = [&](int slab, int buf) {
+            if (slab == whole) {
+                // the last one, that ends early
+                const int k0 = slab * KS;
+                int own = tid;
+                asm volatile("" : "+v"(own));          // what follows of it is made here, not kept in registers through the loop
+#pragma unroll
+                for (int i = 0; i < NA; ++i) {
+                    int row, col;
+                    ex_place<F, COLS_A, BM>(own + i * NT, row, col);
+                    ex_load_lds_from(k0 + (COLS_A ? row : col) < ks ? tile_a + slab * next_a + off_a[i] : (const char *)&ex_nothing, lds + buf * SLAB + i * NT * 16);
+                }
+#pragma unroll
+                for (int i = 0; i < NB; ++i) {
+                    int row, col;
+                    ex_place<F, COLS_B, BN>(own + i * NT, row, col);
+                    ex_load_lds_from(k0 + (COLS_B ? row : col) < ks ? tile_b + slab * next_b + off_b[i] : (const char *)&ex_nothing,
+                                     lds + buf * SLAB + BM * kSlabBytes + i * NT * 16);
+                }
+                if constexpr (MX)
+#pragma unroll
+                    for (int i = 0; i < NSC; ++i) {
+                        sc[i] = 0;
+                        for (int e = 0; e < 8; ++e)
+                            if (slab * 8 + e < blocks) sc[i] |= (unsigned long long)row_s[i][slab * 8 + e] << (8 * e);
+                    }
+                return;
+            }
             const char *pa = tile_a + slab * next_a, *pb = tile_b + slab * next_b;
 #pragma unroll
             for (int i = 0; i < NA; ++i) ex_load_lds(pa, off_a[i], lds + buf * SLAB + i * NT * 16);
@@ -351,20 +390,22 @@ __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_prod
             step(std::integral_constant<int, 2>{});
             step(std::integral_constant<int, 3>{});
         };
-        const int slabs = (ks + KS - 1) / KS, whole = ALIGNED ? ks / KS : 0;
+        if constexpr (ALIGNED) {
 #pragma unroll
-        for (int i = 0; i < STAGES - 1; ++i)
-            if (i < whole) fetch(i, i);
+            for (int i = 0; i < STAGES - 1; ++i)
+                if (i < slabs) fetch(i, i);
+        }
         for (int i = 0, buf = 0; i < slabs; ++i) {
-            if (i < whole) {
-                if (i + STAGES - 1 <= whole) ex_loads_done<(STAGES - 2) * (NA + NB)>();
+            if constexpr (ALIGNED) {
+                if (i + STAGES - 1 <= slabs) ex_loads_done<(STAGES - 2) * (NA + NB)>();
                 else ex_loads_done<0>();
                 if constexpr (MX) put_scales(buf);
             } else {
                 fill(i, buf);
             }
             __syncthreads();
-            if (i + STAGES - 1 < whole) fetch(i + STAGES - 1, buf == 0 ? STAGES - 1 : buf - 1);
+            if constexpr (ALIGNED)
+                if (i + STAGES - 1 < slabs) fetch(i + STAGES - 1, buf == 0 ? STAGES - 1 : buf - 1);
             if (busy) compute(buf);
             buf = buf == STAGES - 1 ? 0 : buf + 1;
         }
@@ -385,7 +426,7 @@ __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_prod
             for (int e = 0; e < 4; ++e) v[e] = has ? acc[i][u][4 * q + e] : 0.f;
         };
         if constexpr (GATED) {
-            ex_put_rows<OUT32, ALIGNED, COLS>(scratch, out, m, n, p.M, p.N, lane, [&](int q, float(&v)[4]) {
+            ex_put_rows<OUT32, ALIGNED, PAST, COLS>(scratch, out, m, n, p.M, p.N, lane, [&](int q, float(&v)[4]) {
                 float w[4];
                 sums(q / 4 * 2, q % 4, v);
                 sums(q / 4 * 2 + 1, q % 4, w);
@@ -397,12 +438,22 @@ __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_prod
                 char *keep = (char *)p.keep + (size_t)j * p.M * n_all * SIZE;
 #pragma unroll
                 for (int half = 0; half < 2; ++half)
-                    ex_put_rows<OUT32, ALIGNED, COLS, 2>(scratch, keep + (size_t)half * p.N * SIZE, m, n, p.M, p.N, lane, [&](int q, float(&v)[4]) { sums(q / 4 * 2 + half, q % 4, v); });
+                    ex_put_rows<OUT32, ALIGNED, PAST, COLS, 2>(scratch, keep + (size_t)half * p.N * SIZE, m, n, p.M, p.N, lane, [&](int q, float(&v)[4]) { sums(q / 4 * 2 + half, q % 4, v); });
             }
         } else {
-            ex_put_rows<OUT32, ALIGNED, COLS>(scratch, out, m, n, p.M, p.N, lane, [&](int q, float(&v)[4]) { sums(q / 4, q % 4, v); });
+            ex_put_rows<OUT32, ALIGNED, PAST, COLS>(scratch, out, m, n, p.M, p.N, lane, [&](int q, float(&v)[4]) { sums(q / 4, q % 4, v); });
         }
     }
+}
+
+// Results beyond the last cache (256 MiB) go past it where there is little to compute for them, eight slabs or, in the weight gradient's 32 bits, sixteen: dW of
+// 64 x 256 rows, 2048 to 1024 in bf16 164 -> 131 us, of 64 x 1024, 1024 to 1024 160 -> 145, four bits 64 x 2048 rows, 2048 to 1024 193 -> 176.  Products of sixteen slabs
+// lose 3 % so, results of half that size 8 %.
+template <int F>
+bool ex_past_caches(const ExpertArgs &p, bool wgrad, bool out32, int outs)
+{
+    constexpr int KS = kSlabBytes / 16 * ExpertElem<F>::chunk;
+    return (size_t)p.E * p.M * p.N * outs * (out32 ? 4 : 2) >= (size_t)256 << 20 && p.K <= (wgrad ? 16 : 8) * KS;
 }
 
 // The tiles of a call and their shares for the dies; whether a launch counts so many threads (32 bits).
@@ -417,14 +468,14 @@ bool ex_divide(ExpertArgs &p, int bm, int bn, int threads, long long &tiles)
     return tiles <= 0xffffffffll / threads;
 }
 
-template <int F, bool COLS_B, bool WGRAD, int END, bool ALIGNED, int WM, int WN, int TM, int TN, int STAGES, int WGS>
+template <int F, bool COLS_B, bool WGRAD, int END, bool ALIGNED, int WM, int WN, int TM, int TN, int STAGES, int WGS, bool PAST = false>
 int32_t ex_launch(ExpertArgs p, hipStream_t s)
 {
     constexpr bool GATED = END == kExpSwiglu || END == kExpSwigluKeep;
     constexpr int BM = 32 * WM * TM, BN = 32 * WN * TN / (GATED ? 2 : 1);
     long long tiles;
     if (!ex_divide(p, BM, BN, 64 * WM * WN, tiles)) return MAXSCORE_ERR_SHAPE;
-    hipLaunchKernelGGL((k_expert_product<F, COLS_B, WGRAD, END, ALIGNED, WM, WN, TM, TN, STAGES, WGS>), dim3((unsigned)tiles), dim3(64 * WM * WN), 0, s, p);
+    hipLaunchKernelGGL((k_expert_product<F, COLS_B, WGRAD, END, ALIGNED, WM, WN, TM, TN, STAGES, WGS, PAST>), dim3((unsigned)tiles), dim3(64 * WM * WN), 0, s, p);
     MS_HIP(hipGetLastError());
     return MAXSCORE_OK;
 }
