@@ -12,7 +12,8 @@ namespace {
 // rows are k's, 64 x 256, as long as there are enough of them: 512 bytes in a row of W, not 256 (64 x 40 rows, 2048 to 2 x 1024 through the gated unit 114 us,
 // 105 so; of W [N, K], whose rows come by 128 bytes either way, 113 and 131).
 // fp32 takes 64 x 128 for all rows (its matrix instructions need no more, and fewer rows of a last tile are idle: 9500 of 384 through the gated unit of 2 x 512
-// 323 -> 310 us, 1266 of 1024 to 2 x 256 of 8 experts 75 -> 48), but not for dW, whose tiles are whole (64 experts' 1920 x 832 166 us, 242 so).
+// 323 -> 310 us, 1266 of 1024 to 2 x 256 of 8 experts 75 -> 48), up to 32 rows one block of them (in 64 x 128 half of the matrix cores would be idle and the
+// others the bound: 64 x 5 rows, 1920 to 832 128 -> 91 us), but not for dW, whose tiles are whole (64 experts' 1920 x 832 166 us, 242 so).
 long long ex_tiles(const ExpertArgs &p, int bm, int bn) { return (long long)((p.M + bm - 1) / bm) * ((p.N + bn - 1) / bn) * p.E; }
 
 template <int F, bool COLS_B, bool WGRAD, int END>
@@ -25,6 +26,8 @@ int32_t ex_run(const ExpertArgs &p, hipStream_t s)
         if (p.M <= 64 || F == kExpFp32) {
             if constexpr (F == kExpMx) return ex_launch<F, COLS_B, WGRAD, END, true, 2, 2, 1, 2, 2, 3>(p, s);
             else {
+                if constexpr (F == kExpFp32)
+                    if (p.M <= 32) return ex_launch<F, COLS_B, WGRAD, END, true, 1, 4, 1, GATED ? 2 : 1, GATED ? 2 : 3, 2>(p, s);
                 if constexpr (F == kExpBf16 && COLS_B)
                     if (tiles > 512) return ex_launch<F, COLS_B, WGRAD, END, true, 2, 4, 1, 2, 2, 2>(p, s);
                 return tiles > 256 ? ex_launch<F, COLS_B, WGRAD, END, true, 2, 2, 1, 2, 3, 2>(p, s) : ex_launch<F, COLS_B, WGRAD, END, true, 2, 2, 1, 2, 6, 1>(p, s);
