@@ -43,7 +43,8 @@ __device__ __forceinline__ unsigned short ex_to_bf16(float v)      // to nearest
     return __builtin_bit_cast(unsigned short, (__bf16)v);
 }
 
-// 16 bytes of elements col .. of row `row` of a matrix of `cols` columns, zero where the matrix has none.
+// 16 bytes of elements col .. of row `row` of a matrix of `cols` columns, zero where the matrix has none.  Rows that begin anywhere: all 16 at once
+// where the row has them.
 template <int F, bool ALIGNED>
 __device__ __forceinline__ ex_u32x4 ex_load16(const char *base, int row, int col, int rows, int cols)
 {
@@ -52,17 +53,18 @@ __device__ __forceinline__ ex_u32x4 ex_load16(const char *base, int row, int col
     if (row >= rows || col >= cols) return v;
     const char *p = base + ((size_t)row * cols + col) * 16 / CE;
     if (ALIGNED) return *(const ex_u32x4 *)p;          // rows are whole numbers of chunks then
+    if (col + CE <= cols) {
+        __builtin_memcpy(&v, p, 16);
+        return v;
+    }
     if constexpr (F == kExpFp32) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 3; ++i)
             if (col + i < cols) v[i] = ((const unsigned *)p)[i];
     } else if constexpr (F == kExpBf16) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 7; ++i)
             if (col + i < cols) v[i / 2] |= (unsigned)((const unsigned short *)p)[i] << (i % 2 * 16);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i / 4] |= (unsigned)((const unsigned char *)p)[i] << (i % 4 * 8);
     }
     return v;
 }
@@ -217,8 +219,9 @@ __device__ __forceinline__ void ex_put_rows(char *scratch, void *out, int m, int
 // has both of an h in the same lane and register.
 //
 // STAGES slabs in LDS: the next ones are on their way, past the registers, while the matrix instructions work on this one, and one barrier a slab keeps
-// them apart (a buffer is filled again once all wavefronts are past the barrier behind its use).  A slab that ends early has zeros behind its end; slabs of rows that are no whole numbers of 16 bytes are filled in through registers.  Rows and
-// columns of the tile that the result does not have are copies of its last ones.
+// them apart (a buffer is filled again once all wavefronts are past the barrier behind its use).  A slab that ends early has zeros behind its end; slabs of rows that are no whole numbers of
+// 16 bytes go through registers, the next one's on their way while this one is used.  Rows and columns of the tile that the result does not have are
+// copies of its last ones, or whatever lies there: nothing of them is stored.
 template <int F, bool COLS_B, bool WGRAD, int END, bool ALIGNED, int WM, int WN, int TM, int TN, int STAGES, int WGS, bool PAST = false>
 __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_product(ExpertArgs p)
 {
@@ -340,30 +343,34 @@ __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_prod
             for (int i = 0; i < NSC; ++i)
                 if (tid + i * NT < BM + BN) *(unsigned long long *)(s_mem + STAGES * SLAB + buf * SCALES + (tid + i * NT) * 8) = sc[i];
         };
-        auto fill = [&](int slab, int buf) {
-            char *s_a = s_mem + buf * SLAB, *s_b = s_a + BM * kSlabBytes;
+        // a slab through registers: under way while the one before is used
+        ex_u32x4 held[ALIGNED ? 1 : NA + NB];
+        auto take = [&](int slab) {
             const int k0 = slab * KS;
 #pragma unroll
             for (int i = 0; i < NA; ++i) {
                 int row, col;
                 ex_place<F, COLS_A, BM>(tid + i * NT, row, col);
-                *(ex_u32x4 *)(s_a + (tid + i * NT) * 16) = COLS_A ? ex_load16<F, ALIGNED>(a, k0 + row, m0 + col, ks, p.M) : ex_load16<F, ALIGNED>(a, m0 + row, k0 + col, ms, p.K);
+                held[i] = COLS_A ? ex_load16<F, false>(a, k0 + row, m0 + col, ks, p.M) : ex_load16<F, false>(a, m0 + row, k0 + col, ms, p.K);
             }
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
                 int row, col;
                 ex_place<F, COLS_B, BN>(tid + i * NT, row, col);
-                *(ex_u32x4 *)(s_b + (tid + i * NT) * 16) = COLS_B ? ex_load16<F, ALIGNED>(b, k0 + row, b_index(col), ks, n_all) : ex_load16<F, ALIGNED>(b, b_index(row), k0 + col, n_all, p.K);
+                held[NA + i] = COLS_B ? ex_load16<F, false>(b, k0 + row, b_index(col), ks, n_all) : ex_load16<F, false>(b, b_index(row), k0 + col, n_all, p.K);
             }
-            if constexpr (MX) {
+            if constexpr (MX)
 #pragma unroll
                 for (int i = 0; i < NSC; ++i) {
                     sc[i] = 0;
                     for (int e = 0; e < 8; ++e)
                         if (slab * 8 + e < blocks) sc[i] |= (unsigned long long)row_s[i][slab * 8 + e] << (8 * e);
                 }
-                put_scales(buf);
-            }
+        };
+        auto put_held = [&](int buf) {
+#pragma unroll
+            for (int i = 0; i < NA + NB; ++i) *(ex_u32x4 *)(s_mem + buf * SLAB + (i < NA ? i * NT : (i - NA) * NT + BM * 8) * 16 + tid * 16) = held[i];
+            if constexpr (MX) put_scales(buf);
         };
         const bool busy = m0 + wm * TM * 32 < ms;           // the others have nothing but rows that the result does not have
         auto compute = [&](int buf) {
@@ -394,6 +401,8 @@ __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_prod
 #pragma unroll
             for (int i = 0; i < STAGES - 1; ++i)
                 if (i < slabs) fetch(i, i);
+        } else {
+            take(0);
         }
         for (int i = 0, buf = 0; i < slabs; ++i) {
             if constexpr (ALIGNED) {
@@ -401,11 +410,14 @@ __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_prod
                 else ex_loads_done<0>();
                 if constexpr (MX) put_scales(buf);
             } else {
-                fill(i, buf);
+                put_held(buf);
             }
             __syncthreads();
-            if constexpr (ALIGNED)
+            if constexpr (ALIGNED) {
                 if (i + STAGES - 1 < slabs) fetch(i + STAGES - 1, buf == 0 ? STAGES - 1 : buf - 1);
+            } else {
+                if (i + 1 < slabs) take(i + 1);
+            }
             if (busy) compute(buf);
             buf = buf == STAGES - 1 ? 0 : buf + 1;
         }
