@@ -169,50 +169,42 @@ __device__ __forceinline__ auto ex_pack4(const float (&v)[4])
 
 // A wavefront's 32 rows of COLS columns of the result at row m, column n of `out`, rows of PITCH * cols of which `cols` are its.  A lane has four columns of one row at a time
 // (values(q, v): columns 8 q + 4 (lane / 32) .. of row lane % 32), which would be 32 stores to as many lines; through its part of LDS (chunks turned as in a slab) they
-// become whole lines.  Rows that are no whole numbers of 16 bytes are stored value by value.
+// become whole lines.  Rows that are no whole numbers of 16 bytes take them all the same, wherever they begin, but for their last ones.
 template <bool FP32, bool ALIGNED, bool PAST, int COLS, int PITCH = 1, typename V>
 __device__ __forceinline__ void ex_put_rows(char *scratch, void *out, int m, int n, int rows, int cols, int lane, V values)
 {
-    constexpr int SIZE = FP32 ? 4 : 2, CPR = COLS * SIZE / 16, PER = 16 / SIZE, ALL = 32 * CPR;
-    if constexpr (ALIGNED) {
-        constexpr int TURN = CPR < 8 ? CPR : 8;
-        const int r = lane & 31;
+    constexpr int SIZE = FP32 ? 4 : 2, CPR = COLS * SIZE / 16, PER = 16 / SIZE, ALL = 32 * CPR, TURN = CPR < 8 ? CPR : 8;
+    const int r = lane & 31;
 #pragma unroll
-        for (int q = 0; q < COLS / 8; ++q) {
-            float v[4];
-            values(q, v);
-            const int at = (8 * q + 4 * (lane >> 5)) * SIZE;
-            *(decltype(ex_pack4<FP32>(v)) *)(scratch + r * (CPR * 16) + (((at >> 4) ^ (r >> 1 & (TURN - 1))) << 4) + (at & 15)) = ex_pack4<FP32>(v);
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // the lanes exchange: LDS goes in order, the compiler has to as well
+    for (int q = 0; q < COLS / 8; ++q) {
+        float v[4];
+        values(q, v);
+        const int at = (8 * q + 4 * (lane >> 5)) * SIZE;
+        *(decltype(ex_pack4<FP32>(v)) *)(scratch + r * (CPR * 16) + (((at >> 4) ^ (r >> 1 & (TURN - 1))) << 4) + (at & 15)) = ex_pack4<FP32>(v);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // the lanes exchange: LDS goes in order, the compiler has to as well
 #pragma unroll
-        for (int i = 0; i < ALL; i += 64) {
-            const int row = (i + lane) / CPR, c = (i + lane) % CPR;
-            if (ALL % 64 && i + lane >= ALL) break;
-            const ex_u32x4 x = *(const ex_u32x4 *)(scratch + row * (CPR * 16) + ((c ^ (row >> 1 & (TURN - 1))) << 4));
-            ex_u32x4 *to = (ex_u32x4 *)((char *)out + ((size_t)(m + row) * (PITCH * (size_t)cols) + n + c * PER) * SIZE);
-            if (m + row < rows && n + c * PER < cols) {
-                if (PAST) __builtin_nontemporal_store(x, to);
-                else *to = x;
-            }
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    } else {
-        if (m + (lane & 31) >= rows) return;
+    for (int i = 0; i < ALL; i += 64) {
+        const int row = (i + lane) / CPR, c = (i + lane) % CPR, left = cols - n - c * PER;
+        if (ALL % 64 && i + lane >= ALL) break;
+        const ex_u32x4 x = *(const ex_u32x4 *)(scratch + row * (CPR * 16) + ((c ^ (row >> 1 & (TURN - 1))) << 4));
+        if (m + row >= rows || left <= 0) continue;
+        char *to = (char *)out + ((size_t)(m + row) * (PITCH * (size_t)cols) + n + c * PER) * SIZE;
+        if constexpr (ALIGNED) {
+            if (PAST) __builtin_nontemporal_store(x, (ex_u32x4 *)to);
+            else *(ex_u32x4 *)to = x;
+        } else if (left >= PER) {
+            __builtin_memcpy(to, &x, 16);
+        } else {
 #pragma unroll
-        for (int q = 0; q < COLS / 8; ++q) {
-            float v[4];
-            values(q, v);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int c = n + 8 * q + 4 * (lane >> 5) + e;
-                const size_t at = (size_t)(m + (lane & 31)) * (PITCH * (size_t)cols) + c;
-                if (c >= cols) continue;
-                if constexpr (FP32) ((float *)out)[at] = v[e];
-                else ((unsigned short *)out)[at] = ex_to_bf16(v[e]);
+            for (int e = 0; e < PER - 1; ++e) {
+                if (e >= left) continue;
+                if constexpr (FP32) ((unsigned *)to)[e] = x[e];
+                else ((unsigned short *)to)[e] = (unsigned short)(x[e / 2] >> (e % 2 * 16));
             }
         }
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
 // WM x WN wavefronts, each with TM x TN blocks of 32 x 32.  The gated unit takes gate and up columns by turns of 32, so that a wavefront
@@ -427,7 +419,7 @@ __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_prod
     constexpr int SIZE = OUT32 ? 4 : 2, COLS = GATED ? TN * 16 : TN * 32;
     static_assert(WM * WN * 32 * COLS * SIZE <= sizeof(s_mem), "every wavefront's part");
     char *scratch = s_mem + wave * (32 * COLS * SIZE), *out = (char *)p.out + (size_t)j * p.M * p.N * SIZE;
-    if (ALIGNED) __syncthreads();
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
         const int m = m0 + (wm * TM + i) * 32, n = n0 + wn * COLS;
