@@ -68,11 +68,50 @@ __device__ __forceinline__ float wave_sum(float v)
            (__int_as_float(__builtin_amdgcn_readlane(w, 32)) + __int_as_float(__builtin_amdgcn_readlane(w, 48)));
 }
 
+// 16 bytes of a row of which `left` values are left; not ALIGNED: from any address, and zero (or nothing) beyond the row's end.
+template <bool ALIGNED, bool NT, typename T>
+__device__ __forceinline__ u32x4 get_piece(const T *p, int left)
+{
+    constexpr int PER = 16 / sizeof(T);
+    if constexpr (ALIGNED) return NT ? __builtin_nontemporal_load((const u32x4 *)p) : *(const u32x4 *)p;
+    u32x4 v = {0u, 0u, 0u, 0u};
+    if (left >= PER) {
+        __builtin_memcpy(&v, p, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER - 1; ++i)
+            if (i < left) {
+                if constexpr (sizeof(T) == 2) v[i / 2] |= (unsigned)__builtin_bit_cast(unsigned short, p[i]) << (i % 2 * 16);
+                else v[i] = __builtin_bit_cast(unsigned, p[i]);
+            }
+    }
+    return v;
+}
+template <bool ALIGNED, bool NT, typename T>
+__device__ __forceinline__ void put_piece(u32x4 v, T *p, int left)
+{
+    constexpr int PER = 16 / sizeof(T);
+    if constexpr (ALIGNED) {
+        if (NT) __builtin_nontemporal_store(v, (u32x4 *)p);
+        else *(u32x4 *)p = v;
+    } else if (left >= PER) {
+        __builtin_memcpy(p, &v, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER - 1; ++i)
+            if (i < left) {
+                if constexpr (sizeof(T) == 2) p[i] = (unsigned short)(v[i / 2] >> (i % 2 * 16));
+                else p[i] = __uint_as_float(v[i]);
+            }
+    }
+}
+
 // A wavefront takes a token, or `parts` of them share its slots where there are few tokens.  It has HOLD * 64 pieces of 16 bytes of a row of the buffers in
 // its registers at a time (a piece: eight columns of bf16, four of fp32), the token's dy once for all its slots, which go two at a time so that one's
 // rows are on their way while the other's are used.  Lane s keeps slot s's gate and sum.  Bound by HBM: dy once, rows in, rows out.
 // The workgroups from n_wg on zero the places that hold nothing, an equal share of every expert's.
-template <typename T, int HOLD, bool NT>
+// Rows that are no whole numbers of 16 bytes, or do not begin on them (not ALIGNED), take the same pieces wherever they lie, the last one value by value.
+template <typename T, int HOLD, bool NT, bool ALIGNED>
 __global__ __launch_bounds__(256) void k_combine_backward(const float *__restrict__ dy, const T *__restrict__ expert_out,
                                                           const int32_t *__restrict__ assign, const int32_t *__restrict__ token_pos,
                                                           const float *__restrict__ gates, const int32_t *__restrict__ offsets, int T_, int d, int E,
@@ -80,13 +119,14 @@ __global__ __launch_bounds__(256) void k_combine_backward(const float *__restric
                                                           float *__restrict__ dgates)
 {
     constexpr int PER = 16 / sizeof(T);
-    const int lane = threadIdx.x & 63, pieces = d / PER;
+    const int lane = threadIdx.x & 63, pieces = ALIGNED ? d / PER : (d + PER - 1) / PER;
     if ((int)blockIdx.x >= n_wg) {
         const int j = (blockIdx.x - n_wg) / shares, share = (blockIdx.x - n_wg) % shares;
         const int n = filled_rows(offsets, j, C);
-        const size_t all = (size_t)(C - n) * pieces, from = all * share / shares, to = all * (share + 1) / shares;
-        u32x4 *p = (u32x4 *)(dexpert_out + ((size_t)j * C + n) * d);
-        for (size_t i = from + threadIdx.x; i < to; i += 256) p[i] = u32x4{0u, 0u, 0u, 0u};
+        T *p = dexpert_out + ((size_t)j * C + n) * d;
+        const size_t all = (size_t)(C - n) * d / PER, from = all * share / shares, to = all * (share + 1) / shares, rest = (size_t)(C - n) * d - all * PER;
+        for (size_t i = from + threadIdx.x; i < to; i += 256) put_piece<ALIGNED, NT>(u32x4{0u, 0u, 0u, 0u}, p + i * PER, PER);
+        if (!ALIGNED && share == 0 && threadIdx.x < rest) p[all * PER + threadIdx.x] = (T)0;
         return;
     }
     const unsigned item = blockIdx.x * 4u + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = item / (unsigned)parts, part = item % (unsigned)parts;
@@ -101,30 +141,33 @@ __global__ __launch_bounds__(256) void k_combine_backward(const float *__restric
         gate = gates[at];
         if (expert >= E || row < 0 || row >= C) expert = -1;       // an empty slot, or a place outside the buffer
     }
-    const f32x4 *dyr = (const f32x4 *)(dy + (size_t)i * d);
+    const float *dyr = dy + (size_t)i * d;
     for (int c0 = 0; c0 < pieces; c0 += 64 * HOLD) {
         f32x4 g[HOLD][PER / 4];
 #pragma unroll
         for (int u = 0; u < HOLD; ++u) {
             const int c = c0 + 64 * u + lane;
 #pragma unroll
-            for (int w = 0; w < PER / 4; ++w) g[u][w] = c < pieces ? dyr[(size_t)c * (PER / 4) + w] : f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int w = 0; w < PER / 4; ++w) {
+                const int at = c * PER + 4 * w, left = d - at;
+                g[u][w] = left > 0 ? __builtin_bit_cast(f32x4, get_piece<ALIGNED, false>(dyr + at, left)) : f32x4{0.f, 0.f, 0.f, 0.f};
+            }
         }
         auto fetch = [&](int s, u32x4(&v)[HOLD]) {
             const int e = __builtin_amdgcn_readlane(expert, s);
             if (e < 0) return;
-            const u32x4 *src = (const u32x4 *)expert_out + ((size_t)e * C + __builtin_amdgcn_readlane(row, s)) * pieces;
+            const T *src = expert_out + ((size_t)e * C + __builtin_amdgcn_readlane(row, s)) * d;
 #pragma unroll
             for (int u = 0; u < HOLD; ++u) {
-                const int c = c0 + 64 * u + lane;
-                v[u] = NT ? __builtin_nontemporal_load(src + (c < pieces ? c : pieces - 1)) : src[c < pieces ? c : pieces - 1];
+                const int c = c0 + 64 * u + lane, at = (c < pieces ? c : pieces - 1) * PER;
+                v[u] = get_piece<ALIGNED, NT>(src + at, d - at);
             }
         };
         auto use = [&](int s, const u32x4(&v)[HOLD]) {
             const int e = __builtin_amdgcn_readlane(expert, s);
             if (e < 0) return;
             const float gs = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(gate), s));
-            u32x4 *dst = (u32x4 *)dexpert_out + ((size_t)e * C + __builtin_amdgcn_readlane(row, s)) * pieces;
+            T *dst = dexpert_out + ((size_t)e * C + __builtin_amdgcn_readlane(row, s)) * d;
             float dot = 0.f;
 #pragma unroll
             for (int u = 0; u < HOLD; ++u) {
@@ -147,10 +190,7 @@ __global__ __launch_bounds__(256) void k_combine_backward(const float *__restric
                         out[w] = __float_as_uint(gs * g[u][0][w]);
                     }
                 }
-                if (c < pieces) {
-                    if (NT) __builtin_nontemporal_store(out, dst + c);
-                    else dst[c] = out;
-                }
+                if (c < pieces) put_piece<ALIGNED, NT>(out, dst + c * PER, d - c * PER);
             }
             dot = wave_sum(dot);
             if (lane == s) sum += dot;
@@ -165,41 +205,6 @@ __global__ __launch_bounds__(256) void k_combine_backward(const float *__restric
         }
     }
     if (lane >= s0 && lane < s1) dgates[(size_t)i * k + lane] = sum;
-}
-
-// Rows that are no whole numbers of 16 bytes, or do not begin on them: value by value.
-template <typename T>
-__global__ __launch_bounds__(256) void k_combine_backward_elem(const float *__restrict__ dy, const T *__restrict__ expert_out,
-                                                               const int32_t *__restrict__ assign, const int32_t *__restrict__ token_pos,
-                                                               const float *__restrict__ gates, const int32_t *__restrict__ offsets, int T_, int d,
-                                                               int E, int k, int C, int n_wg, T *__restrict__ dexpert_out, float *__restrict__ dgates)
-{
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if ((int)blockIdx.x >= n_wg) {
-        const int j = blockIdx.x - n_wg, n = filled_rows(offsets, j, C);
-        T *p = dexpert_out + ((size_t)j * C + n) * d;
-        const size_t all = (size_t)(C - n) * d;
-        for (size_t i = threadIdx.x; i < all; i += 256) p[i] = (T)0;
-        return;
-    }
-    const int i = blockIdx.x * 4 + wave;
-    if (i >= T_) return;
-    for (int s = 0; s < k; ++s) {
-        const size_t at = (size_t)i * k + s;
-        const int e = assign[at], pos = token_pos[at];
-        float sum = 0.f;
-        if (e >= 0 && e < E && pos >= 0 && pos < C) {
-            const float g = gates[at];
-            const size_t row = ((size_t)e * C + pos) * d;
-            for (int c = lane; c < d; c += 64) {
-                const float v = dy[(size_t)i * d + c];
-                sum = fmaf(v, to_f32(expert_out[row + c]), sum);
-                dexpert_out[row + c] = from_f32<T>(g * v);
-            }
-            sum = wave_sum(sum);
-        }
-        if (lane == 0) dgates[at] = sum;
-    }
 }
 
 }  // namespace
@@ -232,28 +237,20 @@ int32_t combine_backward_run(const float *dy, const void *expert_out, int dtype,
 {
     const int size = dtype == MAXSCORE_DTYPE_BF16 ? 2 : 4;
     const bool vec = (size_t)d * size % 16 == 0 && (((uintptr_t)dy | (uintptr_t)expert_out | (uintptr_t)dexpert_out) % 16) == 0;
-    if (!vec) {
-        const int n_wg = (T + 3) / 4;
-#define MS_COMBINE_B(TT)                                                                                                                          \
-    hipLaunchKernelGGL((k_combine_backward_elem<TT>), dim3(n_wg + E), dim3(256), 0, s, dy, (const TT *)expert_out, assign, token_pos, gates, offsets, \
-                       T, d, E, k, C, n_wg, (TT *)dexpert_out, dgates)
-        if (size == 2) MS_COMBINE_B(unsigned short);
-        else MS_COMBINE_B(float);
+    // sixteen wavefronts to a compute unit, as far as there are slots
+    const int parts = std::max(1, std::min(k, (4096 + T - 1) / T));
+    const int n_wg = (int)(((long long)T * parts + 3) / 4), shares = std::max(1, 1024 / E);
+    const bool nt = (size_t)E * C * d * size >= (size_t)256 << 20;          // beyond the last cache
+#define MS_COMBINE_B(TT, NN, AA)                                                                                                              \
+    hipLaunchKernelGGL((k_combine_backward<TT, 4, NN, AA>), dim3(n_wg + E * shares), dim3(256), 0, s, dy, (const TT *)expert_out, assign, token_pos, gates, \
+                   offsets, T, d, E, k, C, parts, n_wg, shares, (TT *)dexpert_out, dgates)
+    if (!vec && size == 2) MS_COMBINE_B(unsigned short, false, false);
+    else if (!vec) MS_COMBINE_B(float, false, false);
+    else if (size == 2 && nt) MS_COMBINE_B(unsigned short, true, true);
+    else if (size == 2) MS_COMBINE_B(unsigned short, false, true);
+    else if (nt) MS_COMBINE_B(float, true, true);
+    else MS_COMBINE_B(float, false, true);
 #undef MS_COMBINE_B
-    } else {
-        // sixteen wavefronts to a compute unit, as far as there are slots
-        const int parts = std::max(1, std::min(k, (4096 + T - 1) / T));
-        const int n_wg = (int)(((long long)T * parts + 3) / 4), shares = std::max(1, 1024 / E);
-        const bool nt = (size_t)E * C * d * size >= (size_t)256 << 20;          // beyond the last cache
-#define MS_COMBINE_B(TT, NN)                                                                                                                  \
-    hipLaunchKernelGGL((k_combine_backward<TT, 4, NN>), dim3(n_wg + E * shares), dim3(256), 0, s, dy, (const TT *)expert_out, assign, token_pos, gates, \
-                       offsets, T, d, E, k, C, parts, n_wg, shares, (TT *)dexpert_out, dgates)
-        if (size == 2 && nt) MS_COMBINE_B(unsigned short, true);
-        else if (size == 2) MS_COMBINE_B(unsigned short, false);
-        else if (nt) MS_COMBINE_B(float, true);
-        else MS_COMBINE_B(float, false);
-#undef MS_COMBINE_B
-    }
     MS_HIP(hipGetLastError());
     return MAXSCORE_OK;
 }
