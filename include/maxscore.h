@@ -347,8 +347,8 @@ int32_t maxscore_combine(const void *expert_out, int32_t in_dtype, const int32_t
  * Buffers are [E, C, width] as maxscore_dispatch_tokens fills them: expert j's rows are the first
  * n_j = expert_offsets[j+1] - expert_offsets[j] (cut off at 0 and C) of its C places.  Places from n_j on are never used on the way in, whatever
  * they hold, and are zero on the way out.  E <= 1024, C <= 2^21, widths (K, N, d) <= 2^20, any of them odd; rows that are whole numbers of 16 bytes
- * in 16-byte aligned buffers take the fast path.  Sums are held in fp32 and rounded once.  All of these calls only enqueue work, use no
- * workspace and may be captured into a graph; results do not depend on what else runs.
+ * in 16-byte aligned buffers take the fast path.  Sums are held in fp32 and rounded once.  Results may not overlap operands.  All of these calls
+ * only enqueue work, use no workspace and may be captured into a graph; the same call gives the same bits.
  *
  * maxscore_expert_matmul: y[j, s, :] = x[j, s, :] . W[j].  x [E, C, K], y [E, C, N] and W are of in_dtype (bf16 or fp32); W is [E, K, N], or with
  * transposed != 0 [E, N, K].  The gradient with respect to x is the same call on dy with the other value of `transposed`.

@@ -167,9 +167,10 @@ __device__ __forceinline__ auto ex_pack4(const float (&v)[4])
     else return ex_u32x2{ex_to_bf16(v[0]) | (unsigned)ex_to_bf16(v[1]) << 16, ex_to_bf16(v[2]) | (unsigned)ex_to_bf16(v[3]) << 16};
 }
 
-// A wavefront's 32 rows of COLS columns of the result at row m, column n of `out`, rows of PITCH * cols of which `cols` are its.  A lane has four columns of one row at a time
-// (values(q, v): columns 8 q + 4 (lane / 32) .. of row lane % 32), which would be 32 stores to as many lines; through its part of LDS (chunks turned as in a slab) they
-// become whole lines.  Rows that are no whole numbers of 16 bytes take them all the same, wherever they begin, but for their last ones.
+// A wavefront's 32 rows of COLS columns of the result at row m, column n of `out`, rows of PITCH * cols of which `cols` are its.  A lane has four columns
+// of one row at a time (values(q, v): columns 8 q + 4 (lane / 32) .. of row lane % 32), which would be 32 stores to as many lines; through its part of LDS
+// (chunks turned as in a slab) they become whole lines (64 x 128 rows' dW, 2048 x 1024, 183 us, 125 so).  Rows that are no whole numbers of 16 bytes take
+// them all the same, wherever they begin, but for their last ones.
 template <bool FP32, bool ALIGNED, bool PAST, int COLS, int PITCH = 1, typename V>
 __device__ __forceinline__ void ex_put_rows(char *scratch, void *out, int m, int n, int rows, int cols, int lane, V values)
 {
@@ -211,9 +212,10 @@ __device__ __forceinline__ void ex_put_rows(char *scratch, void *out, int m, int
 // has both of an h in the same lane and register.
 //
 // STAGES slabs in LDS: the next ones are on their way, past the registers, while the matrix instructions work on this one, and one barrier a slab keeps
-// them apart (a buffer is filled again once all wavefronts are past the barrier behind its use).  A slab that ends early has zeros behind its end; slabs of rows that are no whole numbers of
-// 16 bytes go through registers, the next one's on their way while this one is used.  Rows and columns of the tile that the result does not have are
-// copies of its last ones, or whatever lies there: nothing of them is stored.
+// them apart (a buffer is filled again once all wavefronts are past the barrier behind its use).  A slab that ends early has zeros behind its end; slabs
+// of rows that are no whole numbers of 16 bytes go through registers, the next one's on their way while this one is used (64 x 256 rows of bf16, 1001 to
+// 513: 75 us; 311 value by value and one slab after the other).  Rows and columns of the tile that the result does not have are copies of its last ones, or
+// whatever lies there: nothing of them is stored.
 template <int F, bool COLS_B, bool WGRAD, int END, bool ALIGNED, int WM, int WN, int TM, int TN, int STAGES, int WGS, bool PAST = false>
 __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_product(ExpertArgs p)
 {
@@ -442,7 +444,8 @@ __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_prod
                 char *keep = (char *)p.keep + (size_t)j * p.M * n_all * SIZE;
 #pragma unroll
                 for (int half = 0; half < 2; ++half)
-                    ex_put_rows<OUT32, ALIGNED, PAST, COLS, 2>(scratch, keep + (size_t)half * p.N * SIZE, m, n, p.M, p.N, lane, [&](int q, float(&v)[4]) { sums(q / 4 * 2 + half, q % 4, v); });
+                    ex_put_rows<OUT32, ALIGNED, PAST, COLS, 2>(scratch, keep + (size_t)half * p.N * SIZE, m, n, p.M, p.N, lane,
+                                                               [&](int q, float(&v)[4]) { sums(q / 4 * 2 + half, q % 4, v); });
             }
         } else {
             ex_put_rows<OUT32, ALIGNED, PAST, COLS>(scratch, out, m, n, p.M, p.N, lane, [&](int q, float(&v)[4]) { sums(q / 4, q % 4, v); });
@@ -450,9 +453,9 @@ __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_prod
     }
 }
 
-// Results beyond the last cache (256 MiB) go past it where there is little to compute for them, eight slabs or, in the weight gradient's 32 bits, sixteen: dW of
-// 64 x 256 rows, 2048 to 1024 in bf16 164 -> 131 us, of 64 x 1024, 1024 to 1024 160 -> 145, four bits 64 x 2048 rows, 2048 to 1024 193 -> 176.  Products of sixteen slabs
-// lose 3 % so, results of half that size 8 %.
+// Results beyond the last cache (256 MiB) go past it where there is little to compute for them, eight slabs or, in the weight gradient's 32 bits,
+// sixteen: dW of 64 x 256 rows, 2048 to 1024 in bf16 164 -> 131 us, of 64 x 1024, 1024 to 1024 160 -> 145, four bits 64 x 2048 rows, 2048 to 1024
+// 193 -> 176.  Products of sixteen slabs lose 3 % so, results of half that size 8 %.
 template <int F>
 bool ex_past_caches(const ExpertArgs &p, bool wgrad, bool out32, int outs)
 {
