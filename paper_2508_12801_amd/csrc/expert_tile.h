@@ -208,26 +208,28 @@ __device__ __forceinline__ void ex_put_rows(char *scratch, void *out, int m, int
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
-// WM x WN wavefronts, each with TM x TN blocks of 32 x 32.  The gated unit takes gate and up columns by turns of 32, so that a wavefront
-// has both of an h in the same lane and register.
+// WM x WN wavefronts, each with TM x TN blocks of 32 x 32; or one such tile and WK = 4 wavefronts, a step of every slab to each, whose sums meet at the end.
+// The gated unit takes gate and up columns by turns of 32, so that a wavefront has both of an h in the same lane and register.
 //
 // STAGES slabs in LDS: the next ones are on their way, past the registers, while the matrix instructions work on this one, and one barrier a slab keeps
 // them apart (a buffer is filled again once all wavefronts are past the barrier behind its use).  A slab that ends early has zeros behind its end; slabs
 // of rows that are no whole numbers of 16 bytes go through registers, the next one's on their way while this one is used (64 x 256 rows of bf16, 1001 to
 // 513: 75 us; 311 value by value and one slab after the other).  Rows and columns of the tile that the result does not have are copies of its last ones, or
 // whatever lies there: nothing of them is stored.
-template <int F, bool COLS_B, bool WGRAD, int END, bool ALIGNED, int WM, int WN, int TM, int TN, int STAGES, int WGS, bool PAST = false>
-__global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_product(ExpertArgs p)
+template <int F, bool COLS_B, bool WGRAD, int END, bool ALIGNED, int WM, int WN, int TM, int TN, int STAGES, int WGS, bool PAST = false, int WK = 1>
+__global__ __launch_bounds__(64 * WM * WN * WK, WGS * WM * WN * WK / 4) void k_expert_product(ExpertArgs p)
 {
-    constexpr int NT = 64 * WM * WN, BM = 32 * WM * TM, BN = 32 * WN * TN, CE = ExpertElem<F>::chunk, KS = kSlabBytes / 16 * CE;
+    constexpr int NT = 64 * WM * WN * WK, BM = 32 * WM * TM, BN = 32 * WN * TN, CE = ExpertElem<F>::chunk, KS = kSlabBytes / 16 * CE;
     constexpr bool GATED = END == kExpSwiglu || END == kExpSwigluKeep, OUT32 = F == kExpFp32 || END == kExpStoreFp32, MX = F == kExpMx;
     constexpr bool COLS_A = WGRAD;
     constexpr int SLAB = (BM + BN) * kSlabBytes, SCALES = MX ? (BM + BN) * 8 : 0;
     static_assert(!MX || STAGES == 2, "a slab's scales wait in registers for all loads before them");
+    static_assert(WK == 1 || (WK == 4 && WM == 1 && WN == 1), "a tile and its steps' wavefronts");
     static_assert(!GATED || TN % 2 == 0, "gate and up in one wavefront");
     static_assert(BM * 8 % NT == 0 && BN * 8 % NT == 0, "as many loads to every wavefront");
     __shared__ __attribute__((aligned(1024))) char s_mem[STAGES * (SLAB + SCALES)];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wk = WK > 1 ? wave : 0, wm = WK > 1 ? 0 : wave / WN,
+              wn = WK > 1 ? 0 : wave % WN;
 
     // Workgroups go to the eight dies in turn; a die takes `together` neighbouring tiles, whose operands meet in its L2.
     const unsigned die = blockIdx.x & 7u, turn = blockIdx.x >> 3;
@@ -386,10 +388,22 @@ __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_prod
 #pragma unroll
                     for (int u = 0; u < TN; ++u) acc[i][u] = ex_mma<F, KK>(fb[u], fa[i], acc[i][u], vb[u], va[i]);
             };
-            step(std::integral_constant<int, 0>{});
-            step(std::integral_constant<int, 1>{});
-            step(std::integral_constant<int, 2>{});
-            step(std::integral_constant<int, 3>{});
+            if constexpr (WK == 1) {
+                step(std::integral_constant<int, 0>{});
+                step(std::integral_constant<int, 1>{});
+                step(std::integral_constant<int, 2>{});
+                step(std::integral_constant<int, 3>{});
+            } else {
+                // (the step's scales in the lowest byte)
+#pragma unroll
+                for (int i = 0; i < TM; ++i) {
+                    const ExpertFrag<F> fa = ex_fragment<F, COLS_A, BM>(s_a, wm * TM + i, wk, lane);
+#pragma unroll
+                    for (int u = 0; u < TN; ++u)
+                        acc[i][u] = ex_mma<F, 0>(ex_fragment<F, COLS_B, BN>(s_b, wn * TN + u, wk, lane), fa, acc[i][u], (int)((unsigned)vb[u] >> (8 * wk)),
+                                                 (int)((unsigned)va[i] >> (8 * wk)));
+                }
+            }
         };
         if constexpr (ALIGNED) {
 #pragma unroll
@@ -422,6 +436,34 @@ __global__ __launch_bounds__(64 * WM * WN, WGS * WM * WN / 4) void k_expert_prod
     static_assert(WM * WN * 32 * COLS * SIZE <= sizeof(s_mem), "every wavefront's part");
     char *scratch = s_mem + wave * (32 * COLS * SIZE), *out = (char *)p.out + (size_t)j * p.M * p.N * SIZE;
     __syncthreads();
+    if constexpr (WK > 1) {
+        // the steps' sums, in the order of the steps, 32 rows at a time
+        static_assert((WK - 1) * TN * 4096 <= sizeof(s_mem), "32 rows' sums of all wavefronts but the first");
+        ex_f32x4 *part = (ex_f32x4 *)s_mem + lane;
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+#pragma unroll
+            for (int u = 0; u < TN; ++u)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (wk > 0)
+                        part[(((wk - 1) * TN + u) * 4 + q) * 64] = ex_f32x4{acc[i][u][4 * q], acc[i][u][4 * q + 1], acc[i][u][4 * q + 2], acc[i][u][4 * q + 3]};
+            __syncthreads();
+            if (wk == 0)
+#pragma unroll
+                for (int w = 0; w < WK - 1; ++w)
+#pragma unroll
+                    for (int u = 0; u < TN; ++u)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const ex_f32x4 v = part[((w * TN + u) * 4 + q) * 64];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[i][u][4 * q + e] += v[e];
+                        }
+            __syncthreads();
+        }
+        if (wk > 0) return;
+    }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
         const int m = m0 + (wm * TM + i) * 32, n = n0 + wn * COLS;
@@ -475,14 +517,15 @@ bool ex_divide(ExpertArgs &p, int bm, int bn, int threads, long long &tiles)
     return tiles <= 0xffffffffll / threads;
 }
 
-template <int F, bool COLS_B, bool WGRAD, int END, bool ALIGNED, int WM, int WN, int TM, int TN, int STAGES, int WGS, bool PAST = false>
+template <int F, bool COLS_B, bool WGRAD, int END, bool ALIGNED, int WM, int WN, int TM, int TN, int STAGES, int WGS, bool PAST = false, int WK = 1>
 int32_t ex_launch(ExpertArgs p, hipStream_t s)
 {
     constexpr bool GATED = END == kExpSwiglu || END == kExpSwigluKeep;
     constexpr int BM = 32 * WM * TM, BN = 32 * WN * TN / (GATED ? 2 : 1);
     long long tiles;
-    if (!ex_divide(p, BM, BN, 64 * WM * WN, tiles)) return MAXSCORE_ERR_SHAPE;
-    hipLaunchKernelGGL((k_expert_product<F, COLS_B, WGRAD, END, ALIGNED, WM, WN, TM, TN, STAGES, WGS, PAST>), dim3((unsigned)tiles), dim3(64 * WM * WN), 0, s, p);
+    if (!ex_divide(p, BM, BN, 64 * WM * WN * WK, tiles)) return MAXSCORE_ERR_SHAPE;
+    hipLaunchKernelGGL((k_expert_product<F, COLS_B, WGRAD, END, ALIGNED, WM, WN, TM, TN, STAGES, WGS, PAST, WK>), dim3((unsigned)tiles),
+                       dim3(64 * WM * WN * WK), 0, s, p);
     MS_HIP(hipGetLastError());
     return MAXSCORE_OK;
 }
