@@ -344,8 +344,8 @@ template <int F, bool COLS_B, bool WGRAD, int END, bool PAST>
 int32_t ex_launch_big(ExpertArgs p, hipStream_t s)
 {
     constexpr int BN = END == kExpSwiglu || END == kExpSwigluKeep ? 128 : 256;
-    long long tiles;
-    if (!ex_divide(p, 256, BN, 512, tiles)) return MAXSCORE_ERR_SHAPE;
+    const long long tiles = ex_divide(p, 256, BN);
+    if (tiles > 0xffffffffll / 512) return MAXSCORE_ERR_SHAPE;          // a launch counts its threads in 32 bits; no memory holds such results
     hipLaunchKernelGGL((k_expert_big<F, COLS_B, WGRAD, END, PAST>), dim3((unsigned)tiles), dim3(512), 0, s, p);
     MS_HIP(hipGetLastError());
     return MAXSCORE_OK;

@@ -29,6 +29,7 @@ struct ExpertArgs {
     int E, C, M, N, K;               // M = C and K the inner width, or (weight gradient) M and N the widths and K = C
     void *out, *keep;                // [E, M, N]; the gated unit: h [E, M, N] and gate_up [E, M, 2N]
     int mt, nt, together;            // tiles, and how many of them a die takes before the next one's
+    unsigned first;                  // the launch's first workgroup among all of the call's
 };
 
 int32_t expert_product_run(ExpertFormat f, bool cols_b, bool wgrad, ExpertEnd end, const ExpertArgs &args, hipStream_t s);

@@ -232,7 +232,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK, WGS * WM * WN * WK / 4) void k_e
               wn = WK > 1 ? 0 : wave % WN;
 
     // Workgroups go to the eight dies in turn; a die takes `together` neighbouring tiles, whose operands meet in its L2.
-    const unsigned die = blockIdx.x & 7u, turn = blockIdx.x >> 3;
+    const unsigned at = p.first + blockIdx.x, die = at & 7u, turn = at >> 3;
     const unsigned tile = (turn / p.together * 8 + die) * p.together + turn % p.together;
     const int per = p.mt * p.nt, j = tile / per, t = tile - j * per;
     if (j >= p.E) return;
@@ -505,16 +505,15 @@ bool ex_past_caches(const ExpertArgs &p, bool wgrad, bool out32, int outs)
     return (size_t)p.E * p.M * p.N * outs * (out32 ? 4 : 2) >= (size_t)256 << 20 && p.K <= (wgrad ? 16 : 8) * KS;
 }
 
-// The tiles of a call and their shares for the dies; whether a launch counts so many threads (32 bits).
-bool ex_divide(ExpertArgs &p, int bm, int bn, int threads, long long &tiles)
+// The tiles of a call and their shares for the dies.
+long long ex_divide(ExpertArgs &p, int bm, int bn)
 {
     p.mt = (p.M + bm - 1) / bm;
     p.nt = (p.N + bn - 1) / bn;
     const long long real = (long long)p.mt * p.nt * p.E;
     p.together = (int)std::min<long long>(kTilesTogether, (real + 7) / 8);          // few tiles: an equal share to every die
     const long long all = 8 * p.together;
-    tiles = (real + all - 1) / all * all;
-    return tiles <= 0xffffffffll / threads;
+    return (real + all - 1) / all * all;
 }
 
 template <int F, bool COLS_B, bool WGRAD, int END, bool ALIGNED, int WM, int WN, int TM, int TN, int STAGES, int WGS, bool PAST = false, int WK = 1>
@@ -522,15 +521,20 @@ int32_t ex_launch(ExpertArgs p, hipStream_t s)
 {
     constexpr bool GATED = END == kExpSwiglu || END == kExpSwigluKeep;
     constexpr int BM = 32 * WM * TM, BN = 32 * WN * TN / (GATED ? 2 : 1);
-    long long tiles;
-    if (!ex_divide(p, BM, BN, 64 * WM * WN * WK, tiles)) return MAXSCORE_ERR_SHAPE;
-    hipLaunchKernelGGL((k_expert_product<F, COLS_B, WGRAD, END, ALIGNED, WM, WN, TM, TN, STAGES, WGS, PAST, WK>), dim3((unsigned)tiles),
-                       dim3(64 * WM * WN * WK), 0, s, p);
+    constexpr int THREADS = 64 * WM * WN * WK;
+    constexpr long long MOST = (1ll << 31) / THREADS;          // a launch counts its threads in 32 bits
+    const long long tiles = ex_divide(p, BM, BN);
+    if (tiles >> 32) return MAXSCORE_ERR_SHAPE;
+    for (long long from = 0; from < tiles; from += MOST) {
+        p.first = (unsigned)from;
+        hipLaunchKernelGGL((k_expert_product<F, COLS_B, WGRAD, END, ALIGNED, WM, WN, TM, TN, STAGES, WGS, PAST, WK>), dim3((unsigned)std::min(MOST, tiles - from)),
+                           dim3(THREADS), 0, s, p);
+    }
     MS_HIP(hipGetLastError());
     return MAXSCORE_OK;
 }
 
-// Whether all rows of the operands and the results begin on 16 bytes and are whole numbers of them, and a tile's offsets fit 32 bits (gate and up rows
+// Whether all rows of the operands and the results begin on 16 bytes and are whole numbers of them, and a tile's offsets fit 31 bits (gate and up rows
 // are N apart).
 template <int F>
 bool ex_aligned(const ExpertArgs &p, bool cols_b, bool wgrad, bool gated)
@@ -538,7 +542,7 @@ bool ex_aligned(const ExpertArgs &p, bool cols_b, bool wgrad, bool gated)
     constexpr int CE = ExpertElem<F>::chunk;
     const uintptr_t at = (uintptr_t)p.a | (uintptr_t)p.b | (uintptr_t)p.out | (uintptr_t)p.keep;
     if (at % 16 || p.N % (F == kExpMx ? 8 : CE)) return false;
-    if (gated && !cols_b && ((long long)p.N + 256) * p.K * 16 / CE >> 32) return false;
+    if (gated && !cols_b && ((long long)p.N + 256) * p.K * 16 / CE >> 31) return false;
     return wgrad ? p.M % CE == 0 : p.K % CE == 0;
 }
 

@@ -28,7 +28,7 @@ int32_t maxscore_expert_matmul(const void *x, const void *W, int32_t in_dtype, i
     if (!x || !W || !expert_offsets || !y) return MAXSCORE_ERR_NULL;
     if (!buffer_ok(E, C) || !width_ok(K) || !width_ok(N)) return MAXSCORE_ERR_SHAPE;
     if (!dtype_ok(in_dtype)) return MAXSCORE_ERR_DTYPE;
-    const ExpertArgs p = {x, W, nullptr, nullptr, expert_offsets, E, C, C, N, K, y, nullptr, 0, 0, 0};
+    const ExpertArgs p = {x, W, nullptr, nullptr, expert_offsets, E, C, C, N, K, y, nullptr, 0, 0, 0, 0};
     return expert_product_run(format_of(in_dtype), !transposed, false, kExpStore, p, (hipStream_t)stream);
 }
 
@@ -38,7 +38,7 @@ int32_t maxscore_expert_matmul_wgrad(const void *x, const void *dy, int32_t in_d
     if (!x || !dy || !expert_offsets || !dW) return MAXSCORE_ERR_NULL;
     if (!buffer_ok(E, C) || !width_ok(K) || !width_ok(N)) return MAXSCORE_ERR_SHAPE;
     if (!dtype_ok(in_dtype) || !dtype_ok(out_dtype) || (in_dtype == MAXSCORE_DTYPE_FP32 && out_dtype != in_dtype)) return MAXSCORE_ERR_DTYPE;
-    const ExpertArgs p = {x, dy, nullptr, nullptr, expert_offsets, E, C, K, N, C, dW, nullptr, 0, 0, 0};
+    const ExpertArgs p = {x, dy, nullptr, nullptr, expert_offsets, E, C, K, N, C, dW, nullptr, 0, 0, 0, 0};
     return expert_product_run(format_of(in_dtype), true, true, out_dtype == MAXSCORE_DTYPE_FP32 ? kExpStoreFp32 : kExpStore, p, (hipStream_t)stream);
 }
 
@@ -48,7 +48,7 @@ int32_t maxscore_expert_swiglu(const void *x, const void *W, int32_t in_dtype, i
     if (!x || !W || !expert_offsets || !h) return MAXSCORE_ERR_NULL;
     if (!buffer_ok(E, C) || !width_ok(K) || !width_ok(N)) return MAXSCORE_ERR_SHAPE;
     if (!dtype_ok(in_dtype)) return MAXSCORE_ERR_DTYPE;
-    const ExpertArgs p = {x, W, nullptr, nullptr, expert_offsets, E, C, C, N, K, h, gate_up, 0, 0, 0};
+    const ExpertArgs p = {x, W, nullptr, nullptr, expert_offsets, E, C, C, N, K, h, gate_up, 0, 0, 0, 0};
     return expert_product_run(format_of(in_dtype), !transposed, false, gate_up ? kExpSwigluKeep : kExpSwiglu, p, (hipStream_t)stream);
 }
 
@@ -93,7 +93,7 @@ static int32_t mx_product(ExpertEnd end, const void *xq, const void *xs, const v
 {
     if (!xq || !xs || !Wq || !Ws || !offsets || !out) return MAXSCORE_ERR_NULL;
     if (!buffer_ok(E, C) || !width_ok(K) || K % 32 || !width_ok(N)) return MAXSCORE_ERR_SHAPE;
-    const ExpertArgs p = {xq, Wq, (const unsigned char *)xs, (const unsigned char *)Ws, offsets, E, C, C, N, K, out, nullptr, 0, 0, 0};
+    const ExpertArgs p = {xq, Wq, (const unsigned char *)xs, (const unsigned char *)Ws, offsets, E, C, C, N, K, out, nullptr, 0, 0, 0, 0};
     return expert_product_run(kExpMx, false, false, end, p, (hipStream_t)stream);
 }
 

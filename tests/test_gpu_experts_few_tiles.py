@@ -82,3 +82,24 @@ def test_rows_do_not_depend_on_what_the_others_hold(ms):
     assert torch.equal(first[:, ::2], again[:, ::2])
     for _ in range(20):
         assert torch.equal(ms.expert_matmul(x, w, off), first)
+
+
+@pytest.mark.parametrize("gated", [False, True])
+def test_the_most_experts_with_the_widest_rows(ms, gated):
+    """1024 experts' one row to 2^20 columns: more tiles than one launch counts threads for.  One product to a sum: one rounding."""
+    print(f"widest rows gated={gated}", flush=True)
+    E, N = 1024, 1 << 20
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randn(E, 1, 1, generator=gen, device="cuda").bfloat16()
+    w = torch.empty(E, 1, 2 * N if gated else N, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    off = torch.arange(E + 1, device="cuda").int()
+    off[8:] -= 1                                               # expert 7 has no row
+    got = ms.expert_swiglu(x, w, off)["h"] if gated else ms.expert_matmul(x, w, off)
+    for j in (0, 6, 7, 8, 255, 256, 511, 512, 513, 1000, 1022, 1023):
+        y = x[j].double() * w[j].double()
+        if j == 7:
+            y = torch.zeros_like(y)
+        if gated:
+            g, u = y[:, :N], y[:, N:]
+            y = u * (g * torch.sigmoid(g))
+        within(got[j], y, HALF["bf16"] * y.abs() * (1 + 16 * STEP32) + (8 * STEP32 * y.abs() if gated else 0.0) + 2.0 ** -133)
