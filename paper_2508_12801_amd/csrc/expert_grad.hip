@@ -23,51 +23,6 @@ __device__ __forceinline__ int filled_rows(const int32_t *__restrict__ offsets, 
     return cnt < 0 ? 0 : cnt < C ? cnt : C;
 }
 
-// h = u g s, dg = dh u s (1 + g (1 - s)), du = dh g s with s = 1 / (1 + e^-g), all from gate_up's and dh's rounded values in fp32.
-// A thread takes PER neighbouring columns of a row (16 bytes, or one of them where rows are no whole numbers of these); bound by HBM.
-template <typename T, int PER>
-__global__ __launch_bounds__(256) void k_swiglu_backward(const T *__restrict__ gate_up, const T *__restrict__ dh, const int32_t *__restrict__ offsets,
-                                                         unsigned row0, unsigned rows, int C, int N, T *__restrict__ dgate_up, T *__restrict__ h)
-{
-    struct __attribute__((aligned(PER * sizeof(T)))) Piece { T v[PER]; };
-    const unsigned pieces = (unsigned)N / PER, at = blockIdx.x * 256u + threadIdx.x, r = at / pieces;
-    if (r >= rows) return;
-    const unsigned row = row0 + r, n = (at - r * pieces) * PER, j = row / (unsigned)C;
-    const bool has = (int)(row - j * C) < filled_rows(offsets, j, C);
-    const size_t gate_at = (size_t)row * 2 * N + n, dh_at = (size_t)row * N + n;
-    Piece dg = {}, du = {}, hv = {};
-    if (has) {
-        const Piece g = *(const Piece *)(gate_up + gate_at), u = *(const Piece *)(gate_up + gate_at + N), d = *(const Piece *)(dh + dh_at);
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const float gv = to_f32(g.v[i]), uv = to_f32(u.v[i]), dv = to_f32(d.v[i]), s = 1.f / (1.f + expf(-gv)), gs = gv * s;
-            hv.v[i] = from_f32<T>(uv * gs);
-            du.v[i] = from_f32<T>(dv * gs);
-            dg.v[i] = from_f32<T>(dv * uv * s * fmaf(gv, 1.f - s, 1.f));
-        }
-    }
-    *(Piece *)(dgate_up + gate_at) = dg;
-    *(Piece *)(dgate_up + gate_at + N) = du;
-    if (h) *(Piece *)(h + dh_at) = hv;
-}
-
-// The sum over the wavefront's lanes, as a tree: within sixteen lanes by lane moves, the four rows' sums one by one.
-template <int CTRL>
-__device__ __forceinline__ float add_lane(float v)
-{
-    return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
-}
-__device__ __forceinline__ float wave_sum(float v)
-{
-    v = add_lane<0xb1>(v);       // quads
-    v = add_lane<0x4e>(v);
-    v = add_lane<0x141>(v);      // halves of a row mirrored, then the row
-    v = add_lane<0x140>(v);
-    const int w = __float_as_int(v);
-    return (__int_as_float(__builtin_amdgcn_readlane(w, 0)) + __int_as_float(__builtin_amdgcn_readlane(w, 16))) +
-           (__int_as_float(__builtin_amdgcn_readlane(w, 32)) + __int_as_float(__builtin_amdgcn_readlane(w, 48)));
-}
-
 // 16 bytes of a row of which `left` values are left; not ALIGNED: from any address, and zero (or nothing) beyond the row's end.
 template <bool ALIGNED, bool NT, typename T>
 __device__ __forceinline__ u32x4 get_piece(const T *p, int left)
@@ -104,6 +59,56 @@ __device__ __forceinline__ void put_piece(u32x4 v, T *p, int left)
                 else p[i] = __uint_as_float(v[i]);
             }
     }
+}
+
+// h = u g s, dg = dh u s (1 + g (1 - s)), du = dh g s with s = 1 / (1 + e^-g), all from gate_up's and dh's rounded values in fp32.
+// A thread takes 16 bytes of neighbouring columns of a row, wherever they lie and the row's last ones value by value where rows are no whole numbers of
+// these (not ALIGNED); bound by HBM (bf16, 64 x 1024 rows of 512 73 us, 5.5 TB/s; 128 x 4096 of 1001 1295, 2253 value by value; fp32 2892 and 2738).
+template <typename T, bool ALIGNED>
+__global__ __launch_bounds__(256) void k_swiglu_backward(const T *__restrict__ gate_up, const T *__restrict__ dh, const int32_t *__restrict__ offsets,
+                                                         unsigned row0, unsigned rows, int C, int N, T *__restrict__ dgate_up, T *__restrict__ h)
+{
+    constexpr int PER = 16 / sizeof(T);
+    struct Piece { T v[PER]; };
+    const unsigned pieces = ((unsigned)N + PER - 1) / PER, at = blockIdx.x * 256u + threadIdx.x, r = at / pieces;
+    if (r >= rows) return;
+    const unsigned row = row0 + r, n = (at - r * pieces) * PER, j = row / (unsigned)C;
+    const int left = N - (int)n;
+    const bool has = (int)(row - j * C) < filled_rows(offsets, j, C);
+    const size_t gate_at = (size_t)row * 2 * N + n, dh_at = (size_t)row * N + n;
+    Piece dg = {}, du = {}, hv = {};
+    if (has) {
+        const Piece g = __builtin_bit_cast(Piece, get_piece<ALIGNED, false>(gate_up + gate_at, left)),
+                    u = __builtin_bit_cast(Piece, get_piece<ALIGNED, false>(gate_up + gate_at + N, left)),
+                    d = __builtin_bit_cast(Piece, get_piece<ALIGNED, false>(dh + dh_at, left));
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const float gv = to_f32(g.v[i]), uv = to_f32(u.v[i]), dv = to_f32(d.v[i]), s = 1.f / (1.f + expf(-gv)), gs = gv * s;
+            hv.v[i] = from_f32<T>(uv * gs);
+            du.v[i] = from_f32<T>(dv * gs);
+            dg.v[i] = from_f32<T>(dv * uv * s * fmaf(gv, 1.f - s, 1.f));
+        }
+    }
+    put_piece<ALIGNED, false>(__builtin_bit_cast(u32x4, dg), dgate_up + gate_at, left);
+    put_piece<ALIGNED, false>(__builtin_bit_cast(u32x4, du), dgate_up + gate_at + N, left);
+    if (h) put_piece<ALIGNED, false>(__builtin_bit_cast(u32x4, hv), h + dh_at, left);
+}
+
+// The sum over the wavefront's lanes, as a tree: within sixteen lanes by lane moves, the four rows' sums one by one.
+template <int CTRL>
+__device__ __forceinline__ float add_lane(float v)
+{
+    return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float wave_sum(float v)
+{
+    v = add_lane<0xb1>(v);       // quads
+    v = add_lane<0x4e>(v);
+    v = add_lane<0x141>(v);      // halves of a row mirrored, then the row
+    v = add_lane<0x140>(v);
+    const int w = __float_as_int(v);
+    return (__int_as_float(__builtin_amdgcn_readlane(w, 0)) + __int_as_float(__builtin_amdgcn_readlane(w, 16))) +
+           (__int_as_float(__builtin_amdgcn_readlane(w, 32)) + __int_as_float(__builtin_amdgcn_readlane(w, 48)));
 }
 
 // A wavefront takes a token, or `parts` of them share its slots where there are few tokens.  It has HOLD * 64 pieces of 16 bytes of a row of the buffers in
@@ -214,17 +219,17 @@ int32_t swiglu_backward_run(const void *gate_up, const void *dh, int dtype, cons
 {
     const int size = dtype == MAXSCORE_DTYPE_BF16 ? 2 : 4;
     const bool vec = (size_t)N * size % 16 == 0 && (((uintptr_t)gate_up | (uintptr_t)dh | (uintptr_t)dgate_up | (uintptr_t)h) % 16) == 0;
-    const unsigned rows = (unsigned)E * (unsigned)C, pieces = vec ? N * size / 16 : N;      // E <= 2^10, C <= 2^21
+    const unsigned rows = (unsigned)E * (unsigned)C, pieces = (N * size + 15) / 16;      // E <= 2^10, C <= 2^21
     const unsigned most = (1u << 31) / pieces;                                             // rows a launch (its threads are counted in 32 bits)
     for (unsigned r0 = 0; r0 < rows; r0 += most) {
         const unsigned n = std::min(most, rows - r0);
-#define MS_SWIGLU_B(TT, PP)                                                                                                                     \
-    hipLaunchKernelGGL((k_swiglu_backward<TT, PP>), dim3((unsigned)(((size_t)n * pieces + 255) / 256)), dim3(256), 0, s, (const TT *)gate_up,       \
+#define MS_SWIGLU_B(TT, AA)                                                                                                                     \
+    hipLaunchKernelGGL((k_swiglu_backward<TT, AA>), dim3((unsigned)(((size_t)n * pieces + 255) / 256)), dim3(256), 0, s, (const TT *)gate_up,       \
                        (const TT *)dh, offsets, r0, n, C, N, (TT *)dgate_up, (TT *)h)
-        if (size == 2 && vec) MS_SWIGLU_B(unsigned short, 8);
-        else if (size == 2) MS_SWIGLU_B(unsigned short, 1);
-        else if (vec) MS_SWIGLU_B(float, 4);
-        else MS_SWIGLU_B(float, 1);
+        if (size == 2 && vec) MS_SWIGLU_B(unsigned short, true);
+        else if (size == 2) MS_SWIGLU_B(unsigned short, false);
+        else if (vec) MS_SWIGLU_B(float, true);
+        else MS_SWIGLU_B(float, false);
 #undef MS_SWIGLU_B
         if (rows - r0 <= most) break;                       // (r0 + most may pass 32 bits)
     }
