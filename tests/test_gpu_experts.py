@@ -1,4 +1,4 @@
-"""GPU parity of the experts' products, the gated unit, their gradients and combine's gradient against the 64-bit checker.
+"""GPU parity of the experts' products, the gated unit, their gradients and combine's gradient against the 64-bit oracle.
 
 Tolerances.  A product of two bf16 or of two four-bit numbers is exact in fp32; a product of fp32 numbers and every addition is off by at most a step
 of fp32, 2^-23 of its result (half a step where it is rounded to nearest), so a sum of K products is within (K + 1) 2^-23 of the sum of the products'
@@ -276,7 +276,7 @@ def test_infinities_and_nans_stay_in_their_rows_and_columns(ms):
 
 @pytest.mark.parametrize("E,C,K,N,dtype", [(16, 512, 1024, 1024, "bf16"), (8, 300, 1000, 504, "fp32"), (64, 40, 2048, 512, "bf16"), (4, 2048, 2048, 512, "bf16")])
 def test_products_of_layers(ms, E, C, K, N, dtype):
-    """Sizes of layers, the checker in 64 bits on the GPU."""
+    """Sizes of layers, the oracle in 64 bits on the GPU."""
     print(f"layers E={E} C={C} K={K} N={N} {dtype}", flush=True)
     gen = torch.Generator(device="cuda").manual_seed(C)
     counts = torch.randint(0, C + 1, (E,), generator=gen, device="cuda")

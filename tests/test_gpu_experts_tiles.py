@@ -189,8 +189,8 @@ def test_every_row_of_one_expert(ms):
         within(dw[full], want, HALF["fp32"] * want.abs() + (C + 1) * STEP32 * (x[full].double().abs().T.contiguous() @ y[full].double().abs()))
 
 
-def test_the_checker_agrees_with_the_products_above():
-    """The 64-bit products used here against the checker's, on one small case."""
+def test_the_oracle_agrees_with_the_products_above():
+    """The 64-bit products used here against the oracle's, on one small case."""
     rng = np.random.default_rng(0)
     x, w = rng.normal(size=(3, 4, 5)), rng.normal(size=(3, 5, 6))
     y, _ = ox.expert_matmul(x, w, np.array([0, 4, 8, 12]))

@@ -1,4 +1,4 @@
-"""Pins of the checker's expert products, gated unit, gradients and four-bit rows: closed forms, double loops and central differences."""
+"""Pins of the oracle's expert products, gated unit, gradients and four-bit rows: closed forms, double loops and central differences."""
 import numpy as np
 import pytest
 
