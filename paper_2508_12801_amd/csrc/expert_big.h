@@ -323,7 +323,7 @@ __global__ __launch_bounds__(512, 2) void k_expert_big(ExpertArgs p)
                     sums(0, q, v);
                     sums(1, q, w);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = ex_silu_times(v[e], w[e]);
+                    for (int e = 0; e < 4; ++e) v[e] = ex_times_silu(ex_sigmoid(v[e]), w[e]);
                 });
                 if constexpr (END == kExpSwigluKeep) {
                     char *keep = (char *)p.keep + (size_t)j * p.M * n_all * SIZE;

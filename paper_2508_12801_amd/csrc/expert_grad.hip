@@ -2,6 +2,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "expert_silu.h"
 #include "expert_steps.h"
 
 namespace maxscore {
@@ -61,9 +62,10 @@ __device__ __forceinline__ void put_piece(u32x4 v, T *p, int left)
     }
 }
 
-// h = u g s, dg = dh u s (1 + g (1 - s)), du = dh g s with s = 1 / (1 + e^-g), all from gate_up's and dh's rounded values in fp32.
+// h = u g s, dg = dh u s (1 + g (1 - s)), du = dh g s with s = 1 / (1 + e^-g), all from gate_up's and dh's rounded values in fp32.  Where that would be left
+// on the way, far below zero or by the product dh u, the powers of two of s and of the factors go apart, so that only results leave it.
 // A thread takes 16 bytes of neighbouring columns of a row, wherever they lie and the row's last ones value by value where rows are no whole numbers of
-// these (not ALIGNED); bound by HBM (bf16, 64 x 1024 rows of 512 73 us, 5.5 TB/s; 128 x 4096 of 1001 1295, 2253 value by value; fp32 2892 and 2738).
+// these (not ALIGNED); bound by HBM (bf16, 64 x 1024 rows of 512 72 us, 5.6 TB/s; 128 x 4096 of 1001 1290, fp32 2925).
 template <typename T, bool ALIGNED>
 __global__ __launch_bounds__(256) void k_swiglu_backward(const T *__restrict__ gate_up, const T *__restrict__ dh, const int32_t *__restrict__ offsets,
                                                          unsigned row0, unsigned rows, int C, int N, T *__restrict__ dgate_up, T *__restrict__ h)
@@ -81,12 +83,28 @@ __global__ __launch_bounds__(256) void k_swiglu_backward(const T *__restrict__ g
         const Piece g = __builtin_bit_cast(Piece, get_piece<ALIGNED, false>(gate_up + gate_at, left)),
                     u = __builtin_bit_cast(Piece, get_piece<ALIGNED, false>(gate_up + gate_at + N, left)),
                     d = __builtin_bit_cast(Piece, get_piece<ALIGNED, false>(dh + dh_at, left));
+        float low = 0.f, top = 0.f;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const float gv = to_f32(g.v[i]), uv = to_f32(u.v[i]), dv = to_f32(d.v[i]), s = 1.f / (1.f + expf(-gv)), gs = gv * s;
+            const float gv = to_f32(g.v[i]), uv = to_f32(u.v[i]), dv = to_f32(d.v[i]), s = ex_near_sigmoid(gv), gs = gv * s, both = dv * uv;
             hv.v[i] = from_f32<T>(uv * gs);
             du.v[i] = from_f32<T>(dv * gs);
-            dg.v[i] = from_f32<T>(dv * uv * s * fmaf(gv, 1.f - s, 1.f));
+            dg.v[i] = from_f32<T>(both * (s * fmaf(gv, 1.f - s, 1.f)));
+            low = fminf(low, gv);
+            top = fmaxf(top, fabsf(both));
+        }
+        if (__builtin_expect(low < kNearGate || top == INFINITY, 0)) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const float gv = to_f32(g.v[i]), uv = to_f32(u.v[i]), dv = to_f32(d.v[i]);
+                if (!(gv < kNearGate || fabsf(dv * uv) == INFINITY)) continue;          // as it is, whatever stands beside it
+                const ExpertSigmoid s = ex_sigmoid(gv);
+                const float slope = s.inverse * fmaf(s.g, 1.f - ldexpf(s.inverse, -s.c), 1.f);
+                hv.v[i] = from_f32<T>(ex_times_silu(s, uv));
+                du.v[i] = from_f32<T>(ex_times_silu(s, dv));
+                dg.v[i] = from_f32<T>(ldexpf(__builtin_amdgcn_frexp_mantf(dv) * __builtin_amdgcn_frexp_mantf(uv) * slope,
+                                             __builtin_amdgcn_frexp_expf(dv) + __builtin_amdgcn_frexp_expf(uv) - s.c));
+            }
         }
     }
     put_piece<ALIGNED, false>(__builtin_bit_cast(u32x4, dg), dgate_up + gate_at, left);

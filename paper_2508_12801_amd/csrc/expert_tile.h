@@ -15,6 +15,7 @@
 #pragma once
 #include <algorithm>
 
+#include "expert_silu.h"
 #include "expert_steps.h"
 
 namespace maxscore {
@@ -155,9 +156,6 @@ __device__ __forceinline__ ex_f32x16 ex_mma(const ExpertFrag<F> &b, const Expert
         return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(bv, av, acc, 4, 4, KK, sb, KK, sa);
     }
 }
-
-// u * g / (1 + e^-g).  Where e^-g is infinite the quotient is zero, as it should be.
-__device__ __forceinline__ float ex_silu_times(float g, float u) { return u * (g / (1.f + expf(-g))); }
 
 // Four neighbouring values as they lie in memory, in fp32 or rounded to bf16.
 template <bool FP32>
@@ -479,7 +477,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK, WGS * WM * WN * WK / 4) void k_e
                 sums(q / 4 * 2, q % 4, v);
                 sums(q / 4 * 2 + 1, q % 4, w);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = ex_silu_times(v[e], w[e]);
+                for (int e = 0; e < 4; ++e) v[e] = ex_times_silu(ex_sigmoid(v[e]), w[e]);
             });
             if constexpr (END == kExpSwigluKeep) {
                 // rows of gate and up are one row of 2 N: gate's columns end at N
