@@ -44,7 +44,7 @@ __global__ __launch_bounds__(512, 2) void k_expert_big(ExpertArgs p)
     __shared__ __attribute__((aligned(1024))) char s_mem[8 * PART + (MX ? 2 * kScalesTwo : 0)];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 2, wn = wave & 3;
 
-    const unsigned die = blockIdx.x & 7u, turn = blockIdx.x >> 3;
+    const unsigned of_all = p.first + blockIdx.x, die = of_all & 7u, turn = of_all >> 3;
     const unsigned tile = (turn / p.together * 8 + die) * p.together + turn % p.together;
     const int per = p.mt * p.nt, j = tile / per, t = tile - j * per;
     if (j >= p.E) return;
@@ -344,9 +344,13 @@ template <int F, bool COLS_B, bool WGRAD, int END, bool PAST>
 int32_t ex_launch_big(ExpertArgs p, hipStream_t s)
 {
     constexpr int BN = END == kExpSwiglu || END == kExpSwigluKeep ? 128 : 256;
+    constexpr long long MOST = (1ll << 31) / 512;          // a launch counts its threads in 32 bits
     const long long tiles = ex_divide(p, 256, BN);
-    if (tiles > 0xffffffffll / 512) return MAXSCORE_ERR_SHAPE;          // a launch counts its threads in 32 bits; no memory holds such results
-    hipLaunchKernelGGL((k_expert_big<F, COLS_B, WGRAD, END, PAST>), dim3((unsigned)tiles), dim3(512), 0, s, p);
+    if (tiles >> 32) return MAXSCORE_ERR_SHAPE;            // (no memory holds the results: 2^37 values an expert at least)
+    for (long long from = 0; from < tiles; from += MOST) {
+        p.first = (unsigned)from;
+        hipLaunchKernelGGL((k_expert_big<F, COLS_B, WGRAD, END, PAST>), dim3((unsigned)std::min(MOST, tiles - from)), dim3(512), 0, s, p);
+    }
     MS_HIP(hipGetLastError());
     return MAXSCORE_OK;
 }
