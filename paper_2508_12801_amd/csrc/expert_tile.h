@@ -72,15 +72,20 @@ __device__ __forceinline__ ex_u32x4 ex_load16(const char *base, int row, int col
 
 // 16 bytes a lane from base + off straight into LDS, a wavefront's 1024 bytes behind each other from `lds` on.  Not waited for: what
 // reads them comes behind ex_loads_done and a barrier.
+// (m0 is named though the compiler hands it out to nothing, of which it warns: a value that it puts there for an instruction of its own may not be taken for
+// one that lasts past this.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void ex_load_lds(const char *base, unsigned off, unsigned lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
 // The same from an address of its own for every lane.
 __device__ __forceinline__ void ex_load_lds_from(const char *at, unsigned lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(at) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(at) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 // What a slab that ends early has behind its end.
 __device__ const ex_u32x4 ex_nothing = {0u, 0u, 0u, 0u};
 // Waits until no more than LEFT of the wavefront's loads are on their way: they end in the order in which they began.
