@@ -65,7 +65,10 @@ int32_t ex_run(const ExpertArgs &p, hipStream_t s)
             // (scales of four bits by four bytes and more at a time)
             if (ex_tiles(p, 256, GATED ? 128 : 256) >= 256 && (F != kExpMx || (p.K % 128 == 0 && (((uintptr_t)p.sa | (uintptr_t)p.sb) & 3) == 0)))
                 return past ? ex_launch_big<F, COLS_B, WGRAD, END, true>(p, s) : ex_launch_big<F, COLS_B, WGRAD, END, false>(p, s);
-        return past ? ex_launch<F, COLS_B, WGRAD, END, true, 2, 2, 2, 2, 2, 2, true>(p, s) : ex_launch<F, COLS_B, WGRAD, END, true, 2, 2, 2, 2, 2, 2>(p, s);
+        // (bf16 comes here with less than 64 MiB of results: fewer than 256 tiles of 256 x 256)
+        if constexpr (F != kExpBf16)
+            if (past) return ex_launch<F, COLS_B, WGRAD, END, true, 2, 2, 2, 2, 2, 2, true>(p, s);
+        return ex_launch<F, COLS_B, WGRAD, END, true, 2, 2, 2, 2, 2, 2>(p, s);
     }
 }
 
