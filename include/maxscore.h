@@ -360,7 +360,9 @@ int32_t maxscore_combine(const void *expert_out, int32_t in_dtype, const int32_t
  * columns first; h [E, C, N]; gate_up [E, C, 2N] receives [g | u] and may be NULL.  h is made from the sums before they are rounded.
  *
  * maxscore_expert_swiglu_backward: from gate_up and dh [E, C, N] (in_dtype, as are the results) dgate_up [E, C, 2N]:
- *   s = 1 / (1 + e^-g),  dg = dh * u * s * (1 + g * (1 - s)),  du = dh * g * s;  h (may be NULL) receives u * g * s again.
+ *   s = 1 / (1 + e^-g),  dg = dh * u * s * (1 + g * (1 - s)),  du = dh * g * s;  h (may be NULL) receives u * g * s.
+ * That h is for the weight gradient of the product behind the unit, for a program that did not keep maxscore_expert_swiglu's.  In bf16 the two may differ in
+ * their last bits: here from g and u as rounded in gate_up, there from their sums.  The kept one is what the product has seen, and the better one if there.
  *
  * maxscore_combine_backward: the gradients of maxscore_combine with respect to the experts' rows and the gates, from dy [T, d] (fp32):
  *   dexpert_out[assign[i, s], token_pos[i, s], :] = gates[i, s] * dy[i, :],   dgates[i, s] = <dy[i, :], expert_out[assign[i, s], token_pos[i, s], :]>.

@@ -656,7 +656,9 @@ def expert_swiglu(x, w, expert_offsets, transposed: bool = False, want_gate_up: 
 
 
 def expert_swiglu_backward(gate_up, dh, expert_offsets, want_h: bool = True, out: Optional[dict] = None):
-    """dict(dgate_up [E, C, 2N], h [E, C, N] or None) from gate_up [E, C, 2N] and dh [E, C, N]; h is the gated unit's result made again."""
+    """dict(dgate_up [E, C, 2N], h [E, C, N] or None) from gate_up [E, C, 2N] and dh [E, C, N].  h is u * g / (1 + e^-g)
+    of gate_up's rounded values, for the weight gradient behind the unit where expert_swiglu's h was not kept (which is of the unrounded ones: in bf16 the
+    two may differ in their last bits, and a kept one is what the product has seen)."""
     here = _here()
     E, C, N = _buffer(dh, "dh")
     code = _dtype_code(dh)
