@@ -9,7 +9,7 @@
 //   reads     B1    A1    A0'   B1'   B0    A1    A0'   B0'      (' the next slab's)
 //   asks for what the quarter before has read, two slabs on
 // Loads end in the order in which they began, so each quarter waits until twelve (two a part) are left, and a barrier tells that all wavefronts' have
-// come and that what they have read last is free.  64 x 4096 rows of bf16, 2048 to 2048: 1.84 ms, 1.19 PFLOP/s (the library's batched product 1.79); with two
+// come and that what they have read last is free.  64 x 4096 rows of bf16, 2048 to 2048: 1.86 ms, 1.18 PFLOP/s (the library's batched product 1.84); with two
 // whole slabs in turn 1.99.  Wavefronts' priorities raised for the matrix instructions cost 3 %, reads that may move behind these 5 %.  A workgroup that
 // goes on to its next tile, whose first slabs it asks for before its results leave, gained 3 % with two thirds of the results and lost 5 to 15 % else.
 #pragma once
