@@ -65,7 +65,8 @@ __device__ __forceinline__ void put_piece(u32x4 v, T *p, int left)
 // h = u g s, dg = dh u s (1 + g (1 - s)), du = dh g s with s = 1 / (1 + e^-g), all from gate_up's and dh's rounded values in fp32.  Where that would be left
 // on the way, far below zero or by the product dh u, the powers of two of s and of the factors go apart, so that only results leave it.
 // A thread takes 16 bytes of neighbouring columns of a row, wherever they lie and the row's last ones value by value where rows are no whole numbers of
-// these (not ALIGNED); bound by HBM (bf16, 64 x 1024 rows of 512 72 us, 5.6 TB/s; 128 x 4096 of 1001 1290, fp32 2925).
+// these (not ALIGNED); bound by HBM (bf16, 64 x 1024 rows of 512 72 us, 5.6 TB/s; 128 x 4096 of 1001 1290, 2253 value by value; fp32 2925 and 2738).
+// The second way is a block of its own, not taken as a rule: all values that way cost bf16's rows of odd width 15 % (128 x 1000 of 513 159 us, 182 so).
 template <typename T, bool ALIGNED>
 __global__ __launch_bounds__(256) void k_swiglu_backward(const T *__restrict__ gate_up, const T *__restrict__ dh, const int32_t *__restrict__ offsets,
                                                          unsigned row0, unsigned rows, int C, int N, T *__restrict__ dgate_up, T *__restrict__ h)
